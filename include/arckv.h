@@ -365,6 +365,108 @@ arckv_status arckv_compact_scored(const arckv_problem *prob, const void *K, cons
 arckv_status arckv_assign_stats(const arckv_problem *prob, int32_t t, const void *ws, size_t ws_bytes,
                                 int32_t *stats, hipStream_t stream);
 
+/* ------------------------------------------------------------------ 8-bit cache
+ * Keys and values of P pairs (one sequence and KV head each) in 8 bits, with a
+ * scale for each block of 64 consecutive tokens: a quarter of a float32 cache,
+ * half of a bfloat16 one.  For block b, rows 64 b .. 64 b + 63 of a pair, keys
+ * and values apart, with A the largest magnitude among the rows it holds:
+ *   scale = 2^e, e the smallest whole number >= -100 with A <= M 2^e,
+ *           M = 448 (ARCKV_E4M3) or 127 (ARCKV_INT8);
+ *   code  = x / scale rounded to the nearest code, ties to even;
+ *   the stored value is scale * code.
+ * Scales are powers of two, so the codes do not depend on how they are computed,
+ * a stored value is exact in bfloat16, and storing it again changes nothing.
+ * An error is at most half a step: 2^-4 of the value's magnitude (2^-10 scale for the
+ * smallest) in e4m3, scale / 2 in int8, where a scale is below A / 63.5.  Keys
+ * with outlier channels lose less in e4m3, values of one magnitude less in int8.
+ * A block that holds a non-finite number has a NaN scale and reads as NaN.
+ * (The largest magnitudes, above 2^127, may round to infinity.)
+ *
+ * The caller owns every array and the number of rows that each pair holds
+ * ("length", an int32 device array where it differs between pairs).  Rows behind
+ * a pair's length are never read; they need not be initialised, nor do the
+ * scales and bounds of blocks that hold none. */
+typedef enum { ARCKV_E4M3 = 0, ARCKV_INT8 = 1 } arckv_qformat;
+
+typedef struct {
+  int32_t P;          /* pairs, 1..2^20 */
+  int32_t rows;       /* rows that a pair has room for, 1..2^26; any number, the last block may be short */
+  int32_t d;          /* head dimension; must be 128 */
+  int32_t format;     /* arckv_qformat */
+  void *K, *V;        /* codes [P][rows][128], one byte each, 16-byte aligned */
+  float *K_scale;     /* [P][ceil(rows / 64)] */
+  float *V_scale;
+  void *K_bounds;     /* [P][ceil(rows / 64)][2][128]: each key channel's smallest and largest code in the
+                       * block, 16-byte aligned; NULL where no arckv_select_blocks call will read them */
+} arckv_qcache;
+
+/* Write n rows of keys and values, [P][n][128] float32 or bfloat16 (dtype; 16-byte
+ * aligned), into the cache:
+ *   start [P] device array: the first row to write, or NULL for 0 (clipped to [0, rows]);
+ *   count [P] device array: how many of the pair's n source rows to write, or NULL
+ *         for all (clipped to [0, n]); rows that would lie past the cache's end are dropped.
+ * The pair then holds start + count rows: rows before start are kept, rows from
+ * start on are replaced, what was behind them no longer counts.  A block that is
+ * written from its middle on is scaled anew for all it holds: the rows kept in
+ * it are rounded again if its scale grows (nothing moves if it does not).
+ * Codes behind the written rows stay as they were, as do blocks without new rows.
+ * Needs 1 <= n <= rows.  No workspace, no synchronisation. */
+arckv_status arckv_qcache_write(const arckv_qcache *c, int32_t n, int32_t dtype, const void *K, const void *V,
+                                const int32_t *start, const int32_t *count, hipStream_t stream);
+
+/* Read rows first .. first + n - 1 of every pair, as float32 or bfloat16 (dtype;
+ * both exact), into K and V [P][n][128], 16-byte aligned.  Rows at or past the
+ * pair's length ([P] device array, or NULL: all rows are held) come back as
+ * zeros.  Needs first >= 0, n >= 1, first + n <= rows. */
+arckv_status arckv_qcache_read(const arckv_qcache *c, int32_t first, int32_t n, int32_t dtype, const int32_t *length,
+                               void *K, void *V, hipStream_t stream);
+
+/* The k blocks of each pair that its G query rows can give the largest logits to.
+ * With lo, hi the block's bounds times its scale, the block's score is
+ *   max_g [ s sum_d max(q_gd lo_d, q_gd hi_d) ] + max_j beta_j  (j over the block's rows),
+ * which no logit of a stored key of the block exceeds; -inf for a block that holds
+ * no row, or none with a bias above -inf; NaN for one with a NaN scale.  The sum is
+ * taken in 64 bits, where it is exact unless a query's channels span more than
+ * about 2^30, and the score rounded once to float32.
+ *   Q      [P][G][128] bfloat16, 16-byte aligned, G in 1..16;
+ *   beta   [P][rows] float32, or NULL;
+ *   length [P] device array of rows held (clipped to [0, rows]), or NULL: all;
+ *   scores [P][ceil(rows / 64)] float32 output;
+ *   blocks [P][k] int32 output: the chosen blocks, ascending, in arckv_select's
+ *          order of scores (ties to the lower block), 1 <= k <= ceil(rows / 64).
+ * Reads scales and bounds, not the codes (c->K, V and V_scale may be NULL).  A
+ * pair with fewer than k blocks in use gets unused ones too, which
+ * arckv_attend_qcache passes over. */
+arckv_status arckv_select_blocks(const arckv_qcache *c, int32_t G, float scale, const void *Q, const float *beta,
+                                 const int32_t *length, int32_t k, float *scores, int32_t *blocks,
+                                 hipStream_t stream);
+
+/* Decode attention over the 8-bit cache, or over listed blocks of it only,
+ * followed by an optional uncompressed block: for each pair and each of its G
+ * query rows,
+ *   out = softmax([s q K^T + beta, s q K_f^T]) [V; V_f]
+ * with K, V the stored values.  arckv_attend's counterpart; over
+ * (C_k, beta, C_v) written by arckv_qcache_write it is the consumer of a
+ * compaction in 8 bits.
+ *   Q        [P][G][128] bfloat16, G in 1..16.
+ *   beta     [P][rows] float32, or NULL for zero bias.  A row with beta = -inf is
+ *            left out, whatever its key and value hold.
+ *   length   [P] device array of rows held (clipped to [0, rows]), or NULL: all.
+ *   blocks   [P][nsel] device array of blocks to attend to, or NULL with nsel = 0
+ *            for all.  Entries outside [0, ceil(rows / 64)) are passed over (a
+ *            list may be padded with -1); a block that is listed twice counts twice.
+ *   K_f, V_f [P][F][128] bfloat16 (may be NULL when F = 0).
+ *   length_f [P] device array of rows held in K_f, V_f (clipped to [0, F]), or NULL: F.
+ *   out      [P][G][128] float32; zeros for a pair without any row to attend to.
+ * All tensors 16-byte aligned (per-pair int32 and float32 arrays by element).
+ * Workspace: arckv_attend_qcache_workspace_size bytes.  Reads every code once. */
+arckv_status arckv_attend_qcache_workspace_size(int32_t P, int32_t rows, int32_t G, int32_t nsel, int32_t F,
+                                                size_t *bytes);
+arckv_status arckv_attend_qcache(const arckv_qcache *c, int32_t G, int32_t nsel, int32_t F, float scale, const void *Q,
+                                 const float *beta, const int32_t *length, const int32_t *blocks, const void *K_f,
+                                 const void *V_f, const int32_t *length_f, float *out, void *ws, size_t ws_bytes,
+                                 hipStream_t stream);
+
 /* Human-readable name of a status code (static string). */
 const char *arckv_status_string(arckv_status s);
 

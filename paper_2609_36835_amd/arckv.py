@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -19,6 +19,8 @@ LIB_PATH = os.path.join(_PKG, "libarckv.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
+E4M3, INT8 = 0, 1
+QBLOCK = 64          # tokens of an 8-bit cache that share a scale
 
 # Every entry point declared in include/arckv.h.
 ENTRY_POINTS = (
@@ -27,7 +29,8 @@ ENTRY_POINTS = (
     "arckv_status_string", "arckv_set_timing", "arckv_stage_times", "arckv_reset_timing",
     "arckv_attend_workspace_size", "arckv_attend", "arckv_budgets", "arckv_select_count", "arckv_select_ex",
     "arckv_dsa_workspace_size", "arckv_score_dsa", "arckv_compact_scored", "arckv_assign_stats",
-    "arckv_attend_noalloc",
+    "arckv_attend_noalloc", "arckv_qcache_write", "arckv_qcache_read", "arckv_select_blocks",
+    "arckv_attend_qcache_workspace_size", "arckv_attend_qcache",
 )
 
 
@@ -62,6 +65,12 @@ class DSAIndexer(ctypes.Structure):
                 ("L_k", ctypes.c_void_p), ("L_x", ctypes.c_void_p), ("b_x", ctypes.c_void_p),
                 ("U_q", ctypes.c_void_p), ("U_k", ctypes.c_void_p), ("U_v", ctypes.c_void_p),
                 ("L_c", ctypes.c_void_p), ("L_v", ctypes.c_void_p)]
+
+
+class QCacheStruct(ctypes.Structure):
+    _fields_ = [("P", ctypes.c_int32), ("rows", ctypes.c_int32), ("d", ctypes.c_int32), ("format", ctypes.c_int32),
+                ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p),
+                ("V_scale", ctypes.c_void_p), ("K_bounds", ctypes.c_void_p)]
 
 
 _LIB = None
@@ -103,6 +112,12 @@ def lib():
                                            vp, vp, vp, vp, vp, vp, sz, vp]
         L.arckv_attend.argtypes = [i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.arckv_attend_noalloc.argtypes = [i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp]
+        QC = P(QCacheStruct)
+        L.arckv_qcache_write.argtypes = [QC, i32, i32, vp, vp, vp, vp, vp]
+        L.arckv_qcache_read.argtypes = [QC, i32, i32, i32, vp, vp, vp, vp]
+        L.arckv_select_blocks.argtypes = [QC, i32, ctypes.c_float, vp, vp, vp, i32, vp, vp, vp]
+        L.arckv_attend_qcache_workspace_size.argtypes = [i32, i32, i32, i32, i32, P(sz)]
+        L.arckv_attend_qcache.argtypes = [QC, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.arckv_assign_stats.argtypes = [P(Problem), i32, vp, sz, vp, vp]
         for name in ENTRY_POINTS:
             getattr(L, name).restype = ctypes.c_int if name != "arckv_status_string" else ctypes.c_char_p
@@ -436,6 +451,137 @@ def compact(K, V, Q, W1, b1, w2, b2, rho, scale=None, params: Optional[FitParams
     c = Compactor(B, T, Q.shape[1], rho, K.dtype, K.device, scale, params)
     out = c(K, V, Q, W1, b1, w2, b2)
     return (*out, c.assign_stats()) if return_stats else out
+
+
+class QCache(NamedTuple):
+    """The arrays of an 8-bit cache (arckv_qcache).  The functions below take any tuple of these five."""
+    K: torch.Tensor                     # codes [P][rows][128], float8_e4m3fn or int8
+    V: torch.Tensor
+    K_scale: torch.Tensor               # [P][ceil(rows / 64)] float32
+    V_scale: torch.Tensor
+    K_bounds: Optional[torch.Tensor]    # [P][ceil(rows / 64)][2][128], the codes' type; None: no select_blocks
+
+
+def qcache(P: int, rows: int, dtype=torch.float8_e4m3fn, device="cuda", bounds: bool = True) -> QCache:
+    """An 8-bit cache for P pairs of up to `rows` rows, nothing written yet (the arrays are uninitialised)."""
+    _qformat(dtype)
+    n = -(-int(rows) // QBLOCK)
+    codes = lambda *s: torch.empty(s, dtype=dtype, device=device)
+    scale = lambda: torch.empty(P, n, dtype=torch.float32, device=device)
+    return QCache(codes(P, rows, 128), codes(P, rows, 128), scale(), scale(), codes(P, n, 2, 128) if bounds else None)
+
+
+def _qformat(dtype: torch.dtype) -> int:
+    if dtype == torch.float8_e4m3fn:
+        return E4M3
+    if dtype == torch.int8:
+        return INT8
+    raise TypeError(f"unsupported cache dtype {dtype}")
+
+
+def _qptr(x: Optional[torch.Tensor], shape, dtype: torch.dtype, device: int, what: str):
+    """Pointer of a tensor that has to have this shape and type and live on the current device."""
+    if x is None:
+        return None
+    if x.dtype != dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {x.dtype}")
+    if x.shape != shape:
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    if x.get_device() != device:
+        raise ValueError(f"{what}: tensors must live on the current GPU")
+    if not x.is_contiguous():
+        raise ValueError(f"{what}: tensors must be contiguous")
+    return x.data_ptr()
+
+
+def _qcache(c) -> tuple:
+    """(struct, P, rows, current device) of a cache tuple."""
+    K, V, Ks, Vs, bounds = c
+    P, rows, d = K.shape
+    dev = torch.cuda.current_device()
+    n = -(-rows // QBLOCK)
+    return QCacheStruct(P, rows, d, _qformat(K.dtype), _qptr(K, K.shape, K.dtype, dev, "K"),
+                        _qptr(V, K.shape, K.dtype, dev, "V"), _qptr(Ks, (P, n), torch.float32, dev, "K_scale"),
+                        _qptr(Vs, (P, n), torch.float32, dev, "V_scale"),
+                        _qptr(bounds, (P, n, 2, d), K.dtype, dev, "K_bounds")), P, rows, dev
+
+
+def qcache_write(cache, K, V, start=None, count=None) -> None:
+    """arckv_qcache_write: rows K, V [P][n][128] (f32 or bf16) into the cache from row start[p] on, the first count[p]
+    of them (int32 [P] on the GPU; None: from row 0, all n)."""
+    st, P, rows, dev = _qcache(cache)
+    n = K.shape[1]
+    _check(lib().arckv_qcache_write(ctypes.byref(st), n, _dtype_code(K.dtype), _qptr(K, (P, n, 128), K.dtype, dev, "K"),
+                                    _qptr(V, (P, n, 128), K.dtype, dev, "V"),
+                                    _qptr(start, (P,), torch.int32, dev, "start"),
+                                    _qptr(count, (P,), torch.int32, dev, "count"), _stream()), "arckv_qcache_write")
+
+
+def qcache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bfloat16, length=None):
+    """arckv_qcache_read: rows first .. first + n - 1 as (K, V) [P][n][128] of dtype (f32 or bf16); zeros from row
+    length[p] (int32 [P]) on."""
+    st, P, rows, dev = _qcache(cache)
+    n = rows - int(first) if n is None else int(n)
+    code = _dtype_code(dtype)
+    K, V = torch.empty(2, P, max(n, 0), 128, dtype=dtype, device=cache[0].device)
+    _check(lib().arckv_qcache_read(ctypes.byref(st), int(first), n, code, _qptr(length, (P,), torch.int32, dev, "length"),
+                                   K.data_ptr(), V.data_ptr(), _stream()), "arckv_qcache_read")
+    return K, V
+
+
+def select_blocks(Q, cache, k: int, beta=None, length=None, scale=None):
+    """arckv_select_blocks: (blocks [P][k] int32 ascending, scores [P][ceil(rows / 64)]) for queries Q [P][G][128]
+    bf16, beta [P][rows] f32 or None, length [P] int32 or None."""
+    st, P, rows, dev = _qcache(cache)
+    G, n = Q.shape[1], -(-rows // QBLOCK)
+    scores = torch.empty(P, n, dtype=torch.float32, device=Q.device)
+    blocks = torch.empty(P, max(int(k), 0), dtype=torch.int32, device=Q.device)
+    _check(lib().arckv_select_blocks(ctypes.byref(st), G, float(scale) if scale else 0.0,
+                                     _qptr(Q, (P, G, 128), torch.bfloat16, dev, "Q"),
+                                     _qptr(beta, (P, rows), torch.float32, dev, "beta"),
+                                     _qptr(length, (P,), torch.int32, dev, "length"), int(k), scores.data_ptr(),
+                                     blocks.data_ptr(), _stream()), "arckv_select_blocks")
+    return blocks, scores
+
+
+def attend_qcache_workspace_size(P: int, rows: int, G: int, nsel: int = 0, F: int = 0) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().arckv_attend_qcache_workspace_size(int(P), int(rows), int(G), int(nsel), int(F), ctypes.byref(out)),
+           "arckv_attend_qcache_workspace_size")
+    return out.value
+
+
+def attend_qcache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f=None, blocks=None, scale=None,
+                  out=None, ws=None) -> torch.Tensor:
+    """arckv_attend_qcache: decode attention of Q [P][G][128] bf16 over the cache's rows below length (int32 [P]), or
+    over the listed blocks [P][nsel] int32 of it, with bias beta [P][rows] f32, and over the rows of K_f, V_f
+    [P][F][128] bf16 below length_f.  out [P][G][128] f32 and ws (uint8, attend_qcache_workspace_size bytes, 256-byte
+    aligned) may be given; a workspace must not be shared by calls that may overlap in time."""
+    st, P, rows, dev = _qcache(cache)
+    G = Q.shape[1]
+    F = K_f.shape[1] if K_f is not None else 0
+    nsel = blocks.shape[1] if blocks is not None else 0
+    if blocks is not None and nsel == 0:
+        raise ValueError("blocks: an empty list")
+    if out is None:
+        out = torch.empty(P, G, 128, dtype=torch.float32, device=Q.device)
+    if ws is None:
+        nbytes = attend_qcache_workspace_size(P, rows, G, nsel, F)
+        ws = _workspace(nbytes, Q.device)
+    else:
+        nbytes = ws.numel()
+    _check(lib().arckv_attend_qcache(ctypes.byref(st), G, nsel, F, float(scale) if scale else 0.0,
+                                     _qptr(Q, (P, G, 128), torch.bfloat16, dev, "Q"),
+                                     _qptr(beta, (P, rows), torch.float32, dev, "beta"),
+                                     _qptr(length, (P,), torch.int32, dev, "length"),
+                                     _qptr(blocks, (P, nsel), torch.int32, dev, "blocks"),
+                                     _qptr(K_f, (P, F, 128), torch.bfloat16, dev, "K_f"),
+                                     _qptr(V_f, (P, F, 128), torch.bfloat16, dev, "V_f"),
+                                     _qptr(length_f, (P,), torch.int32, dev, "length_f"),
+                                     _qptr(out, (P, G, 128), torch.float32, dev, "out"),
+                                     _qptr(ws, ws.shape, torch.uint8, dev, "ws"), nbytes, _stream()),
+           "arckv_attend_qcache")
+    return out
 
 
 def set_timing(enable: bool):

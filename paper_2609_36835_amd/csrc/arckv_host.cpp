@@ -11,6 +11,7 @@
 #include "arckv.h"
 #include "assign.hpp"
 #include "fit.hpp"
+#include "qcache.hpp"
 
 namespace arckv {
 typedef uint16_t bf16_t_;   // bfloat16 storage, opaque on the host
@@ -123,17 +124,29 @@ int dsa_query_blocks(int n);
 hipError_t launch_attend(int P, int G, int t, int F, float scale, const void *Q, const void *Ck, const float *beta,
                          const void *Cv, const void *Kf, const void *Vf, float *part_o, float *part_ml, float *out,
                          hipStream_t s);
+hipError_t launch_qcache_write(int fmt, int dtype, const QCache &c, int n, const void *K, const void *V,
+                               const int32_t *start, const int32_t *count, hipStream_t s);
+hipError_t launch_qcache_read(int fmt, int dtype, const QCache &c, int first, int n, const int32_t *length, void *K,
+                              void *V, hipStream_t s);
+hipError_t launch_select_blocks(int fmt, const QCache &c, int G, double scale, const void *Q, const float *beta,
+                                const int32_t *length, int k, float *scores, int32_t *blocks, hipStream_t s);
+int attendq_chunks(int nsel, int F, int *nq);
+hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, const void *Q, const float *beta,
+                          const int32_t *length, const int32_t *blocks, int nsel, const void *Kf, const void *Vf,
+                          const int32_t *length_f, float *part_o, float *part_ml, float *out, hipStream_t s);
 
 // ------------------------------------------------------------------ timing
 enum Stage {
   ST_SCORE, ST_SELECT, ST_ROWSTATS, ST_ZMAX, ST_PROFILES, ST_ANCHOR_PROF, ST_ASSIGN, ST_FINALIZE, ST_MERGE,
   ST_PHIC, ST_GRAM_G, ST_CHOL_G, ST_SOLVE_W, ST_PHAT, ST_GRAM_A, ST_RHS, ST_CHOL_A, ST_SOLVE_V, ST_ATTEND,
-  ST_DSA_PROJ, ST_DSA_VALUE, ST_DSA_INDEX, ST_ASSIGN_REFINE, ST_ASSIGN_EXACT, ST_COUNT
+  ST_DSA_PROJ, ST_DSA_VALUE, ST_DSA_INDEX, ST_ASSIGN_REFINE, ST_ASSIGN_EXACT,
+  ST_QCACHE_WRITE, ST_QCACHE_READ, ST_SELECT_BLOCKS, ST_ATTEND_QCACHE, ST_COUNT
 };
 static const char *kStageNames[ST_COUNT] = {
     "score", "select", "rowstats", "zmax", "profiles", "anchor_profiles", "assign_gemm", "assign_finalize",
     "merge", "phic", "gram_G", "chol_G", "solve_beta", "phat", "gram_A", "rhs_B", "chol_A", "solve_values",
-    "attend", "dsa_proj", "dsa_value_head", "dsa_index", "assign_refine", "assign_exact"};
+    "attend", "dsa_proj", "dsa_value_head", "dsa_index", "assign_refine", "assign_exact",
+    "qcache_write", "qcache_read", "select_blocks", "attend_qcache"};
 
 struct TimingState {
   std::mutex mu;
@@ -984,6 +997,107 @@ arckv_status arckv_compact_scored(const arckv_problem *prob, const void *K, cons
   if (!scores) return ARCKV_ERR_INVALID_ARG;
   return compact_impl(prob, K, V, Q_ref, nullptr, scores, rho, p, t_out, anchors, C_k, beta, C_v, info, ws,
                       ws_bytes, stream);
+}
+
+// ---------------------------------------------------------------- 8-bit cache
+// Rows that the kernels' 32-bit row and chunk indexes cover with room to spare.
+constexpr int32_t kQRowsMax = 1 << 26;
+constexpr int32_t kQPairsMax = 1 << 20;
+
+static arckv_status check_qcache(const arckv_qcache *c, bool data, bool bounds) {
+  if (!c || c->P < 1 || c->rows < 1) return ARCKV_ERR_INVALID_ARG;
+  if (c->d != kHeadDimH || (c->format != ARCKV_E4M3 && c->format != ARCKV_INT8)) return ARCKV_ERR_UNSUPPORTED;
+  if (c->rows > kQRowsMax || c->P > kQPairsMax) return ARCKV_ERR_UNSUPPORTED;
+  if (!c->K_scale || (data && (!c->K || !c->V || !c->V_scale)) || (bounds && !c->K_bounds)) return ARCKV_ERR_INVALID_ARG;
+  if (!aligned(c->K, 16) || !aligned(c->V, 16) || !aligned(c->K_bounds, 16) || !aligned(c->K_scale, 4) ||
+      !aligned(c->V_scale, 4))
+    return ARCKV_ERR_INVALID_ARG;
+  return ARCKV_OK;
+}
+
+static QCache make_qcache(const arckv_qcache *c) {
+  return QCache{(uint8_t *)c->K, (uint8_t *)c->V, c->K_scale, c->V_scale, (uint8_t *)c->K_bounds,
+                c->P, c->rows, (c->rows + kQBlock - 1) / kQBlock};
+}
+
+arckv_status arckv_qcache_write(const arckv_qcache *c, int32_t n, int32_t dtype, const void *K, const void *V,
+                                const int32_t *start, const int32_t *count, hipStream_t stream) {
+  CHECK(check_qcache(c, true, false));
+  if (n < 1 || !K || !V || !aligned(K, 16) || !aligned(V, 16) || !aligned(start, 4) || !aligned(count, 4))
+    return ARCKV_ERR_INVALID_ARG;
+  if (dtype != ARCKV_F32 && dtype != ARCKV_BF16) return ARCKV_ERR_UNSUPPORTED;
+  if (n > kQRowsMax) return ARCKV_ERR_UNSUPPORTED;
+  if (n > c->rows) return ARCKV_ERR_INVALID_ARG;
+  STAGE(ST_QCACHE_WRITE, launch_qcache_write(c->format, dtype, make_qcache(c), n, K, V, start, count, stream));
+  return ARCKV_OK;
+}
+
+arckv_status arckv_qcache_read(const arckv_qcache *c, int32_t first, int32_t n, int32_t dtype, const int32_t *length,
+                               void *K, void *V, hipStream_t stream) {
+  CHECK(check_qcache(c, true, false));
+  if (first < 0 || n < 1 || n > c->rows || first > c->rows - n) return ARCKV_ERR_INVALID_ARG;
+  if (!K || !V || !aligned(K, 16) || !aligned(V, 16) || !aligned(length, 4)) return ARCKV_ERR_INVALID_ARG;
+  if (dtype != ARCKV_F32 && dtype != ARCKV_BF16) return ARCKV_ERR_UNSUPPORTED;
+  STAGE(ST_QCACHE_READ, launch_qcache_read(c->format, dtype, make_qcache(c), first, n, length, K, V, stream));
+  return ARCKV_OK;
+}
+
+arckv_status arckv_select_blocks(const arckv_qcache *c, int32_t G, float scale, const void *Q, const float *beta,
+                                 const int32_t *length, int32_t k, float *scores, int32_t *blocks,
+                                 hipStream_t stream) {
+  CHECK(check_qcache(c, false, true));
+  const QCache q = make_qcache(c);
+  if (G < 1 || k < 1 || k > q.nblk || !Q || !scores || !blocks) return ARCKV_ERR_INVALID_ARG;
+  if (G > 16) return ARCKV_ERR_UNSUPPORTED;
+  if (!isfinite(scale) || !aligned(Q, 16) || !aligned(beta, 4) || !aligned(length, 4) || !aligned(scores, 4) ||
+      !aligned(blocks, 4))
+    return ARCKV_ERR_INVALID_ARG;
+  const double s = scale > 0.0f ? (double)scale : 1.0 / sqrt((double)kHeadDimH);
+  STAGE(ST_SELECT_BLOCKS, launch_select_blocks(c->format, q, G, s, Q, beta, length, k, scores, blocks, stream));
+  return ARCKV_OK;
+}
+
+static arckv_status check_attend_qcache(int32_t P, int32_t rows, int32_t G, int32_t nsel, int32_t F) {
+  if (P < 1 || rows < 1 || G < 1 || nsel < 0 || F < 0) return ARCKV_ERR_INVALID_ARG;
+  if (G > 16 || P > kQPairsMax || rows > kQRowsMax || nsel > kQRowsMax / kQBlock || F > kQRowsMax) return ARCKV_ERR_UNSUPPORTED;
+  return ARCKV_OK;
+}
+
+static size_t attend_qcache_ws_bytes(int32_t P, int32_t rows, int32_t G, int32_t nsel, int32_t F, size_t *ml) {
+  int nq;
+  const size_t nch = (size_t)attendq_chunks(nsel > 0 ? nsel : (rows + kQBlock - 1) / kQBlock, F, &nq);
+  *ml = (size_t)rup((int64_t)((size_t)P * nch * G * kHeadDimH * 4), 256);
+  return nch == 1 ? 256 : *ml + (size_t)rup((int64_t)((size_t)P * nch * G * 2 * 4), 256);
+}
+
+arckv_status arckv_attend_qcache_workspace_size(int32_t P, int32_t rows, int32_t G, int32_t nsel, int32_t F,
+                                                size_t *bytes) {
+  CHECK(check_attend_qcache(P, rows, G, nsel, F));
+  if (!bytes) return ARCKV_ERR_INVALID_ARG;
+  size_t ml;
+  *bytes = attend_qcache_ws_bytes(P, rows, G, nsel, F, &ml);
+  return ARCKV_OK;
+}
+
+arckv_status arckv_attend_qcache(const arckv_qcache *c, int32_t G, int32_t nsel, int32_t F, float scale, const void *Q,
+                                 const float *beta, const int32_t *length, const int32_t *blocks, const void *K_f,
+                                 const void *V_f, const int32_t *length_f, float *out, void *ws, size_t ws_bytes,
+                                 hipStream_t stream) {
+  CHECK(check_qcache(c, true, false));
+  CHECK(check_attend_qcache(c->P, c->rows, G, nsel, F));
+  if (!Q || !out || (nsel > 0 && !blocks) || (nsel == 0 && blocks) || (F > 0 && (!K_f || !V_f)))
+    return ARCKV_ERR_INVALID_ARG;
+  if (!isfinite(scale) || !aligned(Q, 16) || !aligned(beta, 4) || !aligned(length, 4) || !aligned(blocks, 4) ||
+      !aligned(K_f, 16) || !aligned(V_f, 16) || !aligned(length_f, 4) || !aligned(out, 4))
+    return ARCKV_ERR_INVALID_ARG;
+  size_t ml;
+  const size_t need = attend_qcache_ws_bytes(c->P, c->rows, G, nsel, F, &ml);
+  if (!ws || !aligned(ws, 256) || ws_bytes < need) return ARCKV_ERR_WORKSPACE;
+  const float s = scale > 0.0f ? scale : 1.0f / sqrtf((float)kHeadDimH);
+  STAGE(ST_ATTEND_QCACHE,
+        launch_attendq(c->format, make_qcache(c), G, F, s, Q, beta, length, blocks, nsel, F > 0 ? K_f : nullptr,
+                       F > 0 ? V_f : nullptr, length_f, (float *)ws, (float *)((char *)ws + ml), out, stream));
+  return ARCKV_OK;
 }
 
 // ---------------------------------------------------------------- value-aware indexer

@@ -6,26 +6,44 @@
 // none of them gets zeros.
 //
 // HBM-bound: 256 bytes of codes per token.  Split-key in two kernels:
-//   k_attendq_partial  a wave takes one block of 64 tokens (so one key scale
-//                      and one value scale), or 32 rows of the tail.  Codes
-//                      become bf16 in registers, where they are exact, and feed
-//                      MFMA 16x16x32: keys as rows and queries as columns for
-//                      the logits, then the lane that holds a query's
-//                      probabilities is the one that feeds them to P V.  The
-//                      block's scales multiply the logits and the sums.  Eight
-//                      waves' (max, sum, o) are merged in LDS.
+//   k_attendq_partial  a workgroup takes a share of the pair's blocks and of its
+//                      tail, a wave one block of 64 tokens (so one key scale and
+//                      one value scale) or 32 rows of the tail at a time, with a
+//                      running softmax.  Codes become bf16 (keys) and fp16
+//                      (values) in registers, where they are exact, and feed MFMA
+//                      16x16x32: keys as rows and queries as columns for the
+//                      logits, then the lane that holds a query's probabilities
+//                      feeds them to (P V)^T, whose columns are the queries again,
+//                      so the sums sit with their maximum.  The next block's keys
+//                      are loaded once this one's are used up, and so are its
+//                      values: 168 registers, three waves on a SIMD, 8 to 16 KB
+//                      in flight each.  The waves' (max, sum, o) are merged in LDS.
 //   k_attendq_combine  merges the partials of a pair; a call of one chunk per
 //                      pair needs none.
+// 512 pairs of 3277 rows with bias and 256 tail rows take 80 us (6.1 TB/s; 93 us with
+// one block per wave and the tail in workgroups of its own, 145 us with loads
+// under branches), of 8192 to 16384 rows 272 us (6.0 TB/s; 314, 495).  Reading alone
+// reaches 6.9 TB/s.
+#include <type_traits>
+
 #include "qcode.hpp"
 
 namespace arckv {
 
 namespace {
-constexpr int kAqW = 8;               // waves per workgroup
+constexpr int kAqW = 4;               // waves per workgroup
+constexpr int kAqSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
+constexpr int kAqStart = 4;           // cost of a workgroup beside its blocks, in blocks per wave
 constexpr int kAqTail = 32;           // tail rows per wave
+// Bytes of codes above which the values are read as a stream that the caches do not keep: the last-level cache's size.
+constexpr int64_t kAttendKept = (int64_t)256 << 20;
 
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ inline f32x4 mfma16h(bf16x8 a, bf16x8 b, f32x4 c) {   // fp16 values in the fragments
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 union Frag {
@@ -40,12 +58,48 @@ __device__ inline uint32_t lower_halves(uint32_t first, uint32_t second) {
   return __builtin_amdgcn_perm(second, first, 0x05040100u);
 }
 
-// Four codes as two words of two bf16 each; every code is exact in bf16.
-template <int FMT> __device__ inline void to_bf16x4(uint32_t w, uint32_t &first, uint32_t &second) {
-  float y[4];
-  QCode<FMT>::unpack4(w, y);
-  first = upper_halves(__float_as_uint(y[0]), __float_as_uint(y[1]));
-  second = upper_halves(__float_as_uint(y[2]), __float_as_uint(y[3]));
+// Codes as MFMA operands, two to a word: keys as bf16 (the queries' type), values as fp16.  Every code is exact in both.
+template <int FMT> struct Operand;
+
+template <> struct Operand<ARCKV_E4M3> {
+  __device__ static inline void bf16x4(uint32_t w, uint32_t &first, uint32_t &second) {
+    first = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+    second = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+  }
+  __device__ static inline void f16x4(uint32_t w, uint32_t &first, uint32_t &second) {
+    first = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+    second = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+  }
+};
+
+template <> struct Operand<ARCKV_INT8> {
+  __device__ static inline void bf16x4(uint32_t w, uint32_t &first, uint32_t &second) {
+    float y[4];
+    QCode<ARCKV_INT8>::unpack4(w, y);
+    first = upper_halves(__float_as_uint(y[0]), __float_as_uint(y[1]));
+    second = upper_halves(__float_as_uint(y[2]), __float_as_uint(y[3]));
+  }
+  // a byte u below fp16's exponent of 1024 is 1024 + u; with the code's sign bit flipped u is code + 128
+  __device__ static inline void f16x4(uint32_t w, uint32_t &first, uint32_t &second) {
+    const f16x2 off = {(f16)-1152.0f, (f16)-1152.0f};
+    w ^= 0x80808080u;
+    first = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) + off);
+    second = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) + off);
+  }
+};
+
+// Probabilities of 8 keys, times 2^kPShift, as two fp16 terms: 22 bits of the large ones, and 2^-39 of the block's
+// largest where they are small.
+constexpr float kPShift = 15.0f;
+__device__ inline void split_p_f16(const float *p, Frag &h, Frag &l) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f32x2 x = {p[2 * k], p[2 * k + 1]};
+    const f16x2 hi = __builtin_convertvector(x, f16x2);
+    const f32x2 rest = {x[0] - (float)hi[0], x[1] - (float)hi[1]};
+    h.w[k] = __builtin_bit_cast(uint32_t, hi);
+    l.w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, f16x2));
+  }
 }
 
 // Probabilities of 8 keys as three bf16 terms (truncated, so all of one sign) that
@@ -68,24 +122,38 @@ __device__ inline void split_p(const float *p, Frag &h, Frag &m, Frag &l) {
   }
 }
 
-// Softmax of a wave's logits per query (columns r, keys over the lane's N and over g):
-// probabilities in place, maximum and sum returned.  -inf marks keys left out.
-template <int N> __device__ inline void wave_softmax(float (&sv)[N], float &m, float &l) {
-  m = sv[0];
+// One step of a running softmax per query (columns r, keys over the lane's N and over g): turns the logits into
+// probabilities times 2^kPShift relative to the new maximum, takes them up in m and l, and returns what the earlier sums
+// have to be multiplied by.  -inf marks keys left out; any: whether there is one that is not.
+template <int N> __device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any) {
+  float top = sv[0];
 #pragma unroll
-  for (int i = 1; i < N; ++i) m = fmaxf(m, sv[i]);
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  m = fmaxf(m, __shfl_xor(m, 32, 64));
-  const float mref = m == -INFINITY ? 0.0f : m;
-  l = 0.0f;
+  for (int i = 1; i < N; ++i) top = fmaxf(top, sv[i]);
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  any = top != -INFINITY;
+  top = fmaxf(top, m);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  const float keep = __builtin_amdgcn_exp2f((m - ref) * 1.44269504f);
+  float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    sv[i] = __expf(sv[i] - mref);
-    l += sv[i];
+    sv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i] - ref, 1.44269504f, kPShift));
+    sum += sv[i];
   }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  m = top;
+  l = fmaf(l, keep, sum);
+  return keep;
 }
+
+// Bounds-checked reads of `bytes` from p on (wave-uniform): zero behind them.
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000);
+}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 }  // namespace
 
 struct AttendQ {
@@ -100,252 +168,380 @@ struct AttendQ {
   const bf16 *Kf, *Vf;
   const int32_t *length_f;
   float *part_o, *part_ml, *out;
-  int nq, nch;                // chunks over the cache; with the tail's
+  int iters, tail_iters, nch; // blocks and tail units per wave of a chunk; chunks per pair
 };
 
-// A block of 64 tokens, `live` of them in use (1..64).
-template <int FMT>
-__device__ inline void attend_block(const AttendQ &a, int p, int b, int live, const bf16 *Q, float &m, float &l,
-                                    f32x4 (&o)[8]) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  const int64_t row0 = (int64_t)p * a.c.rows + (int64_t)b * kQBlock;
-  // keys as MFMA rows; a contraction step pairs bytes 64 kk + 16 g + 8 h .. + 7 of keys and queries, so that a lane
-  // reads 16 bytes at a time
-  uint4 kc[4][2];
+// What a wave has in flight of a block of 64 tokens.  Keys as MFMA rows, where a contraction step pairs bytes
+// 64 kk + 16 g + 8 h .. + 7 of keys and queries, so that a lane reads 16 bytes at a time; values for the lane of keys
+// 16 (i / 4) + 4 g + i % 4 (those of its logits) and dims 8 r .. 8 r + 7.
+struct Keys {
+  u32x4 c[4][2];
+  float scale, bias;
+};
+struct Values {
+  u32x2 c[16];
+  float scale;
+};
+
+// Loads of block b of pair p, `live` of its tokens in use (both the wave's); none where live is 0, and zeros behind them.
+template <bool BETA>
+__device__ inline void load_keys(const AttendQ &a, int64_t pair_block, int64_t row0, int live, Keys &k) {
+  const int lane = threadIdx.x & 63, at = (lane & 15) * kHeadDim + 16 * (lane >> 4);
+  const __amdgpu_buffer_rsrc_t kb = buffer(a.c.K + row0 * kHeadDim, live * kHeadDim);
 #pragma unroll
-  for (int kt = 0; kt < 4; ++kt) {
-    const uint8_t *row = a.c.K + (row0 + min(16 * kt + r, live - 1)) * kHeadDim + 16 * g;
-    kc[kt][0] = *reinterpret_cast<const uint4 *>(row);
-    kc[kt][1] = *reinterpret_cast<const uint4 *>(row + 64);
-  }
-  bf16x8 qf[4];
+  for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks)
-    qf[ks] = *reinterpret_cast<const bf16x8 *>(Q + (int64_t)min(r, a.G - 1) * kHeadDim + 64 * (ks / 2) + 16 * g + 8 * (ks % 2));
-  const float kscale = a.c.Ks[(int64_t)p * a.c.nblk + b] * a.scale, vscale = a.c.Vs[(int64_t)p * a.c.nblk + b];
-  // values: the lane of keys 16 (i / 4) + 4 g + i % 4 (those of its logits) and dims 8 r .. 8 r + 7
-  uint2 vc[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    vc[i] = *reinterpret_cast<const uint2 *>(a.c.V + (row0 + min(16 * (i / 4) + 4 * g + i % 4, live - 1)) * kHeadDim + 8 * r);
-  float bv[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    bv[i] = a.beta ? a.beta[row0 + min(16 * (i / 4) + 4 * g + i % 4, live - 1)] : 0.0f;
-  float sv[16];
-#pragma unroll
-  for (int kt = 0; kt < 4; ++kt) {
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const uint4 c = kc[kt][ks / 2];
-      Frag k;
-      to_bf16x4<FMT>(ks % 2 ? c.z : c.x, k.w[0], k.w[1]);
-      to_bf16x4<FMT>(ks % 2 ? c.w : c.y, k.w[2], k.w[3]);
-      acc = mfma16(k.v, qf[ks], acc);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = 4 * kt + j;
-      const bool held = 16 * kt + 4 * g + j < live && bv[i] != -INFINITY;
-      sv[i] = held ? fmaf(kscale, acc[j], bv[i]) : -INFINITY;
-      if (!held) vc[i] = make_uint2(0u, 0u);   // its probability is zero, but zero times a NaN code is not
-    }
-  }
-  wave_softmax(sv, m, l);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    Frag ph, pm, pl, vb[8];
-    split_p(sv + 8 * half, ph, pm, pl);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint2 x = vc[8 * half + 2 * k], y = vc[8 * half + 2 * k + 1];
-#pragma unroll
-      for (int dd = 0; dd < 2; ++dd) {
-        // bytes of two keys side by side: dims 4 dd, 4 dd + 1, then 4 dd + 2, 4 dd + 3
-        const uint32_t u = dd ? x.y : x.x, w = dd ? y.y : y.x;
-        to_bf16x4<FMT>(__builtin_amdgcn_perm(w, u, 0x05010400u), vb[4 * dd].w[k], vb[4 * dd + 1].w[k]);
-        to_bf16x4<FMT>(__builtin_amdgcn_perm(w, u, 0x07030602u), vb[4 * dd + 2].w[k], vb[4 * dd + 3].w[k]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = mfma16(ph.v, vb[e].v, mfma16(pm.v, vb[e].v, mfma16(pl.v, vb[e].v, o[e])));
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] *= vscale;
+    for (int kk = 0; kk < 2; ++kk)
+      k.c[kt][kk] = __builtin_amdgcn_raw_buffer_load_b128(kb, at + 16 * kHeadDim * (kt % 2) + 64 * kk, 4096 * (kt / 2), 0);
+  k.scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer(a.c.Ks + pair_block, live ? 4 : 0), 0, 0, 0));
+  if constexpr (BETA)
+    k.bias = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer(a.beta + row0, live * 4), 4 * lane, 0, 0));
 }
 
-// 32 rows of the tail from row0 on, `live` of them in use (1..32).
-__device__ inline void attend_tail(const AttendQ &a, int p, int row0, int live, const bf16 *Q, float &m, float &l,
-                                   f32x4 (&o)[8]) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  const int64_t first = (int64_t)p * a.F + row0;
-  bf16x8 kf[2][4], qf[4];
+template <int NT>
+__device__ inline void load_values(const AttendQ &a, int64_t pair_block, int64_t row0, int live, Values &v) {
+  const int lane = threadIdx.x & 63, at = 4 * (lane >> 4) * kHeadDim + 8 * (lane & 15);
+  const __amdgpu_buffer_rsrc_t vb = buffer(a.c.V + row0 * kHeadDim, live * kHeadDim);
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    v.c[i] = __builtin_amdgcn_raw_buffer_load_b64(vb, at + 16 * kHeadDim * (i / 4 % 2) + kHeadDim * (i % 4), 4096 * (i / 8), NT);
+  v.scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer(a.c.Vs + pair_block, live ? 4 : 0), 0, 0, 0));
+}
+
+// A wave's query operands go to LDS, [step][lane]: a block's 16 products would hold 16 registers for them.
+__device__ inline void put_queries(const bf16x8 (&qf)[4], bf16x8 *s_q) {
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) s_q[ks * 64 + (threadIdx.x & 63)] = qf[ks];
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The blocks first, first + kAqW, ... below end of the list (or of the cache), a wave's share of a chunk.
+template <int FMT, bool BETA, bool STREAM>
+__device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end, int len, float *s_bias,
+                                     const bf16x8 (&qf0)[4], bf16x8 *s_q, float &m, float &l, f32x4 (&o)[8]) {
+  constexpr int NTV = STREAM ? 2 : 0;
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  // block and live tokens of list entry idx; none past the end
+  auto block_at = [&](int idx, int &b, int &live) {
+    b = idx < end ? idx : -1;
+    if (a.blocks && idx < end) b = __builtin_amdgcn_readfirstlane(a.blocks[(int64_t)p * a.nsel + idx]);
+    const bool in = b >= 0 && b < a.c.nblk;
+    live = __builtin_amdgcn_readfirstlane(in ? max(0, min(len - b * kQBlock, kQBlock)) : 0);
+    b = in ? b : 0;
+  };
+  int b, live;
+  block_at(first, b, live);
+  Keys k;
+  Values v;
+  const int64_t pb = (int64_t)p * a.c.nblk, pr = (int64_t)p * a.c.rows;
+  load_keys<BETA>(a, pb + b, pr + (int64_t)b * kQBlock, live, k);
+  load_values<NTV>(a, pb + b, pr + (int64_t)b * kQBlock, live, v);
+  __builtin_amdgcn_sched_barrier(0);
+  put_queries(qf0, s_q);
+  for (int idx = first; idx < end; idx += kAqW) {
+    int nb, nlive;
+    block_at(idx + kAqW, nb, nlive);
+    float bv[16];
+    if constexpr (BETA) {
+      // one load per lane, spread to the lanes of a key's logits through LDS that only this wave uses
+      s_bias[lane] = lane < live ? k.bias : -INFINITY;
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const float4 x = *reinterpret_cast<const float4 *>(s_bias + 16 * kt + 4 * g);
+        bv[4 * kt] = x.x;
+        bv[4 * kt + 1] = x.y;
+        bv[4 * kt + 2] = x.z;
+        bv[4 * kt + 3] = x.w;
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    // ---- logits: lane (g, r) holds keys 16 kt + 4 g + j (j < 4) for query r
+    bf16x8 qf[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) qf[ks] = s_q[ks * 64 + lane];
+    float sv[16];
+    const float kscale = k.scale * a.scale;
+    uint32_t masked = 0;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const u32x4 c = k.c[kt][ks / 2];
+        Frag f;
+        Operand<FMT>::bf16x4(c[2 * (ks % 2)], f.w[0], f.w[1]);
+        Operand<FMT>::bf16x4(c[2 * (ks % 2) + 1], f.w[2], f.w[3]);
+        acc = mfma16(f.v, qf[ks], acc);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * kt + j;
+        if constexpr (BETA) {
+          const bool held = bv[i] != -INFINITY;
+          sv[i] = held ? fmaf(kscale, acc[j], bv[i]) : -INFINITY;
+          masked |= held ? 0u : 1u << i;
+        } else {
+          sv[i] = 16 * kt + 4 * g + j < live ? kscale * acc[j] : -INFINITY;
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys<BETA>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
+    __builtin_amdgcn_sched_barrier(0);
+    bool any;
+    const float keep = softmax_step(sv, m, l, any);
+    if constexpr (BETA) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (masked >> i & 1) v.c[i] = u32x2{0u, 0u};   // its probability is zero, but zero times a NaN code is not
+    }
+    // ---- (P V)^T: the lane's probabilities are column r of the B operand with its keys as contraction slots, and its
+    // values row r of eight A operands, one per dim 8 r + e: the sums of query r end up with its maximum
+    Frag ph[2], pl[2];
+    split_p_f16(sv, ph[0], pl[0]);
+    split_p_f16(sv + 8, ph[1], pl[1]);
+    const float vscale = any ? v.scale : 0.0f;   // of a block that is left out whole it may be NaN
+#pragma unroll
+    for (int dd = 0; dd < 2; ++dd) {
+      f32x4 acc[4] = {};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        Frag vf[4];
+#pragma unroll
+        for (int kq = 0; kq < 4; ++kq) {
+          const uint32_t x = v.c[8 * half + 2 * kq][dd], y = v.c[8 * half + 2 * kq + 1][dd];
+          // bytes of two keys side by side: dims 4 dd, 4 dd + 1, then 4 dd + 2, 4 dd + 3
+          Operand<FMT>::f16x4(__builtin_amdgcn_perm(y, x, 0x05010400u), vf[0].w[kq], vf[1].w[kq]);
+          Operand<FMT>::f16x4(__builtin_amdgcn_perm(y, x, 0x07030602u), vf[2].w[kq], vf[3].w[kq]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = mfma16h(vf[e].v, ph[half].v, mfma16h(vf[e].v, pl[half].v, acc[e]));
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[4 * dd + e][j] = fmaf(vscale, acc[e][j], o[4 * dd + e][j] * keep);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_values<NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, v);
+    __builtin_amdgcn_sched_barrier(0);
+    b = nb;
+    live = nlive;
+  }
+}
+
+// 32 rows of the tail, `live` of them in use: what a wave has in flight of them.  The contraction steps are the blocks',
+// so a lane reads 32 bytes at a time of a key.
+__device__ inline void load_tail_keys(const AttendQ &a, int64_t row0, int live, u32x4 (&k)[2][4]) {
+  const int lane = threadIdx.x & 63, at = (lane & 15) * 2 * kHeadDim + 32 * (lane >> 4);
+  const __amdgpu_buffer_rsrc_t kb = buffer(a.Kf + row0 * kHeadDim, live * 2 * kHeadDim);
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks)
-      kf[kt][ks] = *reinterpret_cast<const bf16x8 *>(a.Kf + (first + min(16 * kt + r, live - 1)) * kHeadDim + 32 * ks + 8 * g);
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks)
-    qf[ks] = *reinterpret_cast<const bf16x8 *>(Q + (int64_t)min(r, a.G - 1) * kHeadDim + 32 * ks + 8 * g);
-  Frag vf[8];
+      k[kt][ks] = __builtin_amdgcn_raw_buffer_load_b128(kb, at + 128 * (ks / 2) + 16 * (ks % 2), 32 * kHeadDim * kt, 0);
+}
+
+template <int NT> __device__ inline void load_tail_values(const AttendQ &a, int64_t row0, int live, u32x4 (&v)[8]) {
+  const int lane = threadIdx.x & 63, at = 4 * (lane >> 4) * 2 * kHeadDim + 16 * (lane & 15);
+  const __amdgpu_buffer_rsrc_t vb = buffer(a.Vf + row0 * kHeadDim, live * 2 * kHeadDim);
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    vf[i].v = *reinterpret_cast<const bf16x8 *>(a.Vf + (first + min(16 * (i / 4) + 4 * g + i % 4, live - 1)) * kHeadDim + 8 * r);
-  float sv[8];
+    v[i] = __builtin_amdgcn_raw_buffer_load_b128(vb, at + 2 * kHeadDim * (i % 4), 32 * kHeadDim * (i / 4), NT);
+}
+
+// The tail's units of 32 rows first, first + kAqW, ... below end, a wave's share of a chunk.
+template <bool STREAM>
+__device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, int len, const bf16x8 *s_q, float &m,
+                                   float &l, f32x4 (&o)[8]) {
+  constexpr int NTV = STREAM ? 2 : 0;
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  const int64_t pr = (int64_t)p * a.F;
+  auto live_at = [&](int idx) { return __builtin_amdgcn_readfirstlane(idx < end ? max(0, min(len - idx * kAqTail, kAqTail)) : 0); };
+  int live = live_at(first);
+  u32x4 k[2][4], v[8];
+  load_tail_keys(a, pr + first * kAqTail, live, k);
+  load_tail_values<NTV>(a, pr + first * kAqTail, live, v);
+  for (int idx = first; idx < end; idx += kAqW) {
+    const int nlive = live_at(idx + kAqW);
+    const int64_t next = pr + (idx + kAqW) * kAqTail;
+    float sv[8];
 #pragma unroll
-  for (int kt = 0; kt < 2; ++kt) {
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int kt = 0; kt < 2; ++kt) {
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) acc = mfma16(kf[kt][ks], qf[ks], acc);
+      for (int ks = 0; ks < 4; ++ks) acc = mfma16(__builtin_bit_cast(bf16x8, k[kt][ks]), s_q[ks * 64 + lane], acc);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = 4 * kt + j;
-      const bool held = 16 * kt + 4 * g + j < live;
-      sv[i] = held ? a.scale * acc[j] : -INFINITY;
-      if (!held) vf[i] = Frag{};   // zero times an infinite value is not zero
+      for (int j = 0; j < 4; ++j) sv[4 * kt + j] = 16 * kt + 4 * g + j < live ? a.scale * acc[j] : -INFINITY;
     }
-  }
-  wave_softmax(sv, m, l);
-  Frag ph, pm, pl;
-  split_p(sv, ph, pm, pl);
+    __builtin_amdgcn_sched_barrier(0);
+    load_tail_keys(a, next, nlive, k);
+    __builtin_amdgcn_sched_barrier(0);
+    bool any;
+    const float keep = softmax_step(sv, m, l, any);
+    Frag ph, pm, pl;
+    split_p(sv, ph, pm, pl);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    Frag b;
+    for (int e = 0; e < 8; ++e) {
+      Frag b;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      b.w[k] = e & 1 ? upper_halves(vf[2 * k].w[e / 2], vf[2 * k + 1].w[e / 2])
-                     : lower_halves(vf[2 * k].w[e / 2], vf[2 * k + 1].w[e / 2]);
-    // the first term has products of its own, which alone carry an infinite value (0 times it in the others is NaN)
-    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    const f32x4 first_term = mfma16(ph.v, b.v, zero), rest = mfma16(pm.v, b.v, mfma16(pl.v, b.v, zero));
+      for (int n = 0; n < 4; ++n)
+        b.w[n] = e & 1 ? upper_halves(v[2 * n][e / 2], v[2 * n + 1][e / 2]) : lower_halves(v[2 * n][e / 2], v[2 * n + 1][e / 2]);
+      // the first term has products of its own, which alone carry an infinite value (0 times it in the others is NaN)
+      const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+      const f32x4 lead = mfma16(b.v, ph.v, zero), rest = mfma16(b.v, pm.v, mfma16(b.v, pl.v, zero));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[e][j] = fabsf(first_term[j]) < INFINITY ? first_term[j] + rest[j] : first_term[j];
+      for (int j = 0; j < 4; ++j) o[e][j] = fmaf(o[e][j], keep, fabsf(lead[j]) < INFINITY ? lead[j] + rest[j] : lead[j]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_tail_values<NTV>(a, next, nlive, v);
+    __builtin_amdgcn_sched_barrier(0);
+    live = nlive;
   }
 }
 
 // GP: the query rows that the LDS has room for, G <= GP <= 16.
-template <int FMT, int GP>
-__global__ void __launch_bounds__(64 * kAqW) k_attendq_partial(AttendQ a) {
+template <int FMT, int GP, bool BETA, bool STREAM>
+__global__ void __launch_bounds__(64 * kAqW, 3) k_attendq_partial(AttendQ a) {
   __shared__ __align__(16) float sO[kAqW][GP][kHeadDim];
   __shared__ float sM[kAqW][GP], sL[kAqW][GP];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
-  const int ch = blockIdx.x;
-  for (int p = blockIdx.y; p < a.c.P; p += gridDim.y) {
-    const int len = clip_len(a.length, p, a.c.rows), len_f = clip_len(a.length_f, p, a.F);
-    const int G = a.G;
-    float m = -INFINITY, l = 0.0f;
-    f32x4 o[8] = {};
-    const bf16 *Q = a.Q + (int64_t)p * G * kHeadDim;
-    bool used;   // whether the combine reads this chunk
-    if (ch < a.nq) {
-      const int idx = ch * kAqW + wave;
-      used = a.blocks || ch * kAqW * kQBlock < len;
-      int b = idx < a.nsel ? idx : -1;
-      if (a.blocks && b >= 0) b = a.blocks[(int64_t)p * a.nsel + idx];
-      const int live = b >= 0 && b < a.c.nblk ? min(len - b * kQBlock, kQBlock) : 0;
-      if (live > 0) attend_block<FMT>(a, p, b, live, Q, m, l, o);
+  __shared__ bf16x8 sQ[kAqW][4 * 64];   // each wave's query operands, [step][lane]
+  __shared__ __align__(16) float sB[BETA ? kAqW : 1][kQBlock];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
+  const int ch = blockIdx.x, p = blockIdx.z * gridDim.y + blockIdx.y, G = a.G;
+  if (p >= a.c.P) return;
+  bf16x8 qf[4];
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+    qf[ks] = *reinterpret_cast<const bf16x8 *>(a.Q + ((int64_t)p * G + min(r, G - 1)) * kHeadDim + 64 * (ks / 2) + 16 * g +
+                                               8 * (ks % 2));
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o[8] = {};
+  {
+    const int len = clip_len(a.length, p, a.c.rows), first = ch * a.iters * kAqW;
+    int end = min(first + a.iters * kAqW, a.nsel);
+    if (!a.blocks) end = min(end, (len + kQBlock - 1) / kQBlock);
+    if (first + wave < end)
+      attend_blocks<FMT, BETA, STREAM>(a, p, first + wave, end, len, sB[BETA ? wave : 0], qf, sQ[wave], m, l, o);
+    else
+      put_queries(qf, sQ[wave]);
+  }
+  if (a.F) {
+    const int len = clip_len(a.length_f, p, a.F), first = ch * a.tail_iters * kAqW;
+    const int end = min(first + a.tail_iters * kAqW, (len + kAqTail - 1) / kAqTail);
+    if (first + wave < end) attend_tail<STREAM>(a, p, first + wave, end, len, sQ[wave], m, l, o);
+  }
+  if (g == 0 && r < G) {
+    sM[wave][r] = m;
+    sL[wave][r] = l;
+  }
+  if (r < G)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float *to = &sO[wave][r][8 * (4 * g + j)];
+      *reinterpret_cast<float4 *>(to) = make_float4(o[0][j], o[1][j], o[2][j], o[3][j]);
+      *reinterpret_cast<float4 *>(to + 4) = make_float4(o[4][j], o[5][j], o[6][j], o[7][j]);
+    }
+  __syncthreads();
+  // one partial (max, sum, o) per query for the chunk; the result itself where there is one chunk
+  for (int idx = tid; idx < G * kHeadDim; idx += 64 * kAqW) {
+    const int q = idx / kHeadDim, dim = idx % kHeadDim;
+    float M = sM[0][q];
+#pragma unroll
+    for (int w = 1; w < kAqW; ++w) M = fmaxf(M, sM[w][q]);
+    float acc = 0.0f, lsum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kAqW; ++w) {
+      if (sM[w][q] == -INFINITY) continue;   // no key in use; its o may be zero times a NaN scale
+      const float f = __expf(sM[w][q] - M);
+      acc = fmaf(f, sO[w][q][dim], acc);
+      lsum = fmaf(f, sL[w][q], lsum);
+    }
+    if (a.nch == 1) {
+      a.out[((int64_t)p * G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
     } else {
-      const int row0 = ((ch - a.nq) * kAqW + wave) * kAqTail;
-      used = (ch - a.nq) * kAqW * kAqTail < len_f;
-      const int live = min(len_f - row0, kAqTail);
-      if (live > 0) attend_tail(a, p, row0, live, Q, m, l, o);
-    }
-    if (!used && a.nch > 1) continue;   // the whole workgroup
-    if (g == 0 && r < G) {
-      sM[wave][r] = m;
-      sL[wave][r] = l;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (4 * g + j < G) {
-        float *to = &sO[wave][4 * g + j][8 * r];
-        *reinterpret_cast<float4 *>(to) = make_float4(o[0][j], o[1][j], o[2][j], o[3][j]);
-        *reinterpret_cast<float4 *>(to + 4) = make_float4(o[4][j], o[5][j], o[6][j], o[7][j]);
-      }
-    __syncthreads();
-    // one partial (max, sum, o) per query for the chunk; the result itself where there is one chunk
-    for (int idx = tid; idx < G * kHeadDim; idx += 64 * kAqW) {
-      const int q = idx / kHeadDim, dim = idx % kHeadDim;
-      float M = sM[0][q];
-#pragma unroll
-      for (int w = 1; w < kAqW; ++w) M = fmaxf(M, sM[w][q]);
-      float acc = 0.0f, lsum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kAqW; ++w) {
-        if (sM[w][q] == -INFINITY) continue;   // no key in use; its o may be zero times a NaN scale
-        const float f = __expf(sM[w][q] - M);
-        acc = fmaf(f, sO[w][q][dim], acc);
-        lsum = fmaf(f, sL[w][q], lsum);
-      }
-      if (a.nch == 1) {
-        a.out[((int64_t)p * G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
-      } else {
-        const int64_t at = ((int64_t)p * a.nch + ch) * G + q;
-        a.part_o[at * kHeadDim + dim] = acc;
-        if (dim == 0) {
-          a.part_ml[2 * at] = M;
-          a.part_ml[2 * at + 1] = lsum;
-        }
+      const int64_t at = ((int64_t)p * a.nch + ch) * G + q;
+      a.part_o[at * kHeadDim + dim] = acc;
+      if (dim == 0) {
+        a.part_ml[2 * at] = M;
+        a.part_ml[2 * at + 1] = lsum;
       }
     }
-    __syncthreads();   // the next pair's chunk uses the same LDS
   }
 }
 
 // One workgroup per (query, pair): thread = dim merges the pair's partials.
 __global__ void __launch_bounds__(kHeadDim) k_attendq_combine(AttendQ a) {
-  const int q = blockIdx.x, dim = threadIdx.x;
-  for (int p = blockIdx.y; p < a.c.P; p += gridDim.y) {
-    const int len = clip_len(a.length, p, a.c.rows), len_f = clip_len(a.length_f, p, a.F);
-    const int n0 = a.blocks ? a.nq : (len + kAqW * kQBlock - 1) / (kAqW * kQBlock);
-    const int n1 = (len_f + kAqW * kAqTail - 1) / (kAqW * kAqTail);
-    const int64_t base = (int64_t)p * a.nch * a.G + q;
-    auto at = [&](int c) { return base + (int64_t)(c < n0 ? c : a.nq + c - n0) * a.G; };
-    float M = -INFINITY;
+  const int q = blockIdx.x, dim = threadIdx.x, p = blockIdx.z * gridDim.y + blockIdx.y;
+  if (p >= a.c.P) return;
+  const float *ml = a.part_ml + ((int64_t)p * a.nch * a.G + q) * 2;
+  const float *po = a.part_o + ((int64_t)p * a.nch * a.G + q) * kHeadDim + dim;
+  float M = -INFINITY;
 #pragma unroll 8
-    for (int c = 0; c < n0 + n1; ++c) M = fmaxf(M, a.part_ml[2 * at(c)]);
-    float acc = 0.0f, lsum = 0.0f;
+  for (int c = 0; c < a.nch; ++c) M = fmaxf(M, ml[(int64_t)c * a.G * 2]);
+  const float ref = M == -INFINITY ? 0.0f : M;
+  float acc = 0.0f, lsum = 0.0f;
 #pragma unroll 8
-    for (int c = 0; c < n0 + n1; ++c) {
-      const float mc = a.part_ml[2 * at(c)];
-      const float f = mc == -INFINITY ? 0.0f : __expf(mc - M);
-      acc = fmaf(f, a.part_o[at(c) * kHeadDim + dim], acc);
-      lsum = fmaf(f, a.part_ml[2 * at(c) + 1], lsum);
-    }
-    a.out[((int64_t)p * a.G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
+  for (int c = 0; c < a.nch; ++c) {
+    const float f = __expf(ml[(int64_t)c * a.G * 2] - ref);   // a chunk without a key in use: zero, as its sums are
+    acc = fmaf(f, po[(int64_t)c * a.G * kHeadDim], acc);
+    lsum = fmaf(f, ml[(int64_t)c * a.G * 2 + 1], lsum);
   }
+  a.out[((int64_t)p * a.G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
 }
 
-// Chunks over the cache's blocks (or the list's) and over the tail.
-int attendq_chunks(int nsel, int F, int *nq) {
-  *nq = (nsel + kAqW - 1) / kAqW;
-  return *nq + (F + kAqW * kAqTail - 1) / (kAqW * kAqTail);
+// Chunks per pair, and each wave's blocks and tail units of one.  Workgroups run kAqSlots at a time, so a call takes as
+// many rounds as they fill, of a workgroup's units and its start each; the number of chunks with the least sum is taken:
+// 512 pairs of 3277 + 256 rows 80 us as one chunk each (96 us as three), of 8192 to 16384 rows 272 us as three.
+int attendq_chunks(int P, int nsel, int F, int *iters, int *tail_iters) {
+  const int nb = (nsel + kAqW - 1) / kAqW, nt = ((F + kAqTail - 1) / kAqTail + kAqW - 1) / kAqW, most = max(nb, nt);
+  auto per = [](int n, int c) { return (n + c - 1) / c; };
+  int best = most;
+  if ((int64_t)P * most > kAqSlots) {
+    int64_t least = INT64_MAX;
+    for (int c = 1; c <= most && (int64_t)P * (c - 1) < 4 * kAqSlots; ++c) {
+      const int64_t rounds = ((int64_t)P * c + kAqSlots - 1) / kAqSlots, cost = rounds * (per(nb, c) + per(nt, c) + kAqStart);
+      if (cost < least) {
+        least = cost;
+        best = c;
+      }
+    }
+  }
+  *iters = per(nb, best);
+  *tail_iters = per(nt, best);
+  return best;
 }
 
 hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const int32_t *blocks, int nsel, const void *Kf, const void *Vf,
                           const int32_t *length_f, float *part_o, float *part_ml, float *out, hipStream_t s) {
   AttendQ a{c, G, F, scale, (const bf16 *)Q, beta, length, blocks, blocks ? nsel : c.nblk, (const bf16 *)Kf,
-            (const bf16 *)Vf, length_f, part_o, part_ml, out, 0, 0};
-  a.nch = attendq_chunks(a.nsel, F, &a.nq);
-  const unsigned py = (unsigned)min(c.P, 65535);
+            (const bf16 *)Vf, length_f, part_o, part_ml, out, 0, 0, 0};
+  a.nch = attendq_chunks(c.P, a.nsel, F, &a.iters, &a.tail_iters);
+  // pairs over y and z: a grid's y extent is limited
+  const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
+  const bool stream = (int64_t)c.P * a.nsel * kQBlock * 2 * kHeadDim > kAttendKept;
   auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py), dim3(64 * kAqW), 0, s, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py, pz), dim3(64 * kAqW), 0, s, a);
     return hipGetLastError();
   };
-  hipError_t e;
-  if (fmt == ARCKV_E4M3)
-    e = G <= 4 ? go(k_attendq_partial<ARCKV_E4M3, 4>)
-               : G <= 8 ? go(k_attendq_partial<ARCKV_E4M3, 8>) : go(k_attendq_partial<ARCKV_E4M3, 16>);
-  else
-    e = G <= 4 ? go(k_attendq_partial<ARCKV_INT8, 4>)
-               : G <= 8 ? go(k_attendq_partial<ARCKV_INT8, 8>) : go(k_attendq_partial<ARCKV_INT8, 16>);
+  auto by_stream = [&](auto fm, auto gp, auto bt) {
+    constexpr int FMT = decltype(fm)::value, GP = decltype(gp)::value;
+    constexpr bool BETA = decltype(bt)::value;
+    return stream ? go(k_attendq_partial<FMT, GP, BETA, true>) : go(k_attendq_partial<FMT, GP, BETA, false>);
+  };
+  auto by_beta = [&](auto fm, auto gp) {
+    return beta ? by_stream(fm, gp, std::true_type{}) : by_stream(fm, gp, std::false_type{});
+  };
+  auto by_rows = [&](auto fm) {
+    return G <= 4 ? by_beta(fm, std::integral_constant<int, 4>{})
+                  : G <= 8 ? by_beta(fm, std::integral_constant<int, 8>{}) : by_beta(fm, std::integral_constant<int, 16>{});
+  };
+  const hipError_t e = fmt == ARCKV_E4M3 ? by_rows(std::integral_constant<int, ARCKV_E4M3>{})
+                                         : by_rows(std::integral_constant<int, ARCKV_INT8>{});
   if (e != hipSuccess || a.nch == 1) return e;
-  hipLaunchKernelGGL(k_attendq_combine, dim3((unsigned)G, py), dim3(kHeadDim), 0, s, a);
+  hipLaunchKernelGGL(k_attendq_combine, dim3((unsigned)G, py, pz), dim3(kHeadDim), 0, s, a);
   return hipGetLastError();
 }
 

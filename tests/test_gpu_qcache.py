@@ -8,8 +8,9 @@ Attention's tolerance, per output element, from its rounding steps (u = 2^-24, L
   - a logit: 128 exact products summed in float32 (the accumulator may truncate: 2u an addition), the scale and the bias:
     |dl| <= s (2 * 128 + 4) u sum_d |q_d k_d| + 2u |l|, and u |l - max| again where the exponential's argument is
     formed in base 2, with 2^-22 for the exponential itself;
-  - a probability is off by that much relatively, so is the sum of them, each adds L rounding steps of u, and P V again;
-  - so |out - ref| <= 2 (D + 3 L' u) sum_j p_j |v_j|, D the largest |dl| + 2^-22, L' = 2 L for the accumulator's steps.
+  - a probability is off by that much relatively, so is the sum of them, each adds L rounding steps of u, and P V again,
+    where a probability enters as two fp16 terms: 2^-22 of it, or 2^-39 of its block's largest;
+  - so |out - ref| <= 2 (D + 3 L' u) sum_j p_j |v_j|, D the largest |dl| + 2^-21, L' = 2 L for the accumulator's steps.
 """
 import math
 
@@ -214,7 +215,7 @@ def attend_bound(Q, K, V, beta, K_f, s, mass_abs):
         b[:len(K)] = np.where(beta > -math.inf, beta, 0)
     sums, l = s * np.abs(Q) @ np.abs(keys).T, s * Q @ keys.T + b
     dl = (2 * 128 + 4) * U * sums + 2 * U * np.abs(l) + U * np.abs(l - l.max(axis=1, keepdims=True))
-    return 2 * (dl.max() + 2.0 ** -22 + 6 * len(keys) * U) * mass_abs + 1e-30
+    return 2 * (dl.max() + 2.0 ** -21 + 6 * len(keys) * U) * mass_abs + 1e-30
 
 
 def check_attend(out, Q, c, fmt, beta, length, K_f, V_f, length_f, blocks, s, pairs=None):

@@ -130,7 +130,7 @@ hipError_t launch_qcache_read(int fmt, int dtype, const QCache &c, int first, in
                               void *V, hipStream_t s);
 hipError_t launch_select_blocks(int fmt, const QCache &c, int G, double scale, const void *Q, const float *beta,
                                 const int32_t *length, int k, float *scores, int32_t *blocks, hipStream_t s);
-int attendq_chunks(int P, int nsel, int F, int *iters, int *tail_iters);
+int attendq_chunks(int P, int nsel, int F, int *iters);
 hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const int32_t *blocks, int nsel, const void *Kf, const void *Vf,
                           const int32_t *length_f, float *part_o, float *part_ml, float *out, hipStream_t s);
@@ -1064,8 +1064,8 @@ static arckv_status check_attend_qcache(int32_t P, int32_t rows, int32_t G, int3
 }
 
 static size_t attend_qcache_ws_bytes(int32_t P, int32_t rows, int32_t G, int32_t nsel, int32_t F, size_t *ml) {
-  int iters, tail_iters;
-  const size_t nch = (size_t)attendq_chunks(P, nsel > 0 ? nsel : (rows + kQBlock - 1) / kQBlock, F, &iters, &tail_iters);
+  int iters;
+  const size_t nch = (size_t)attendq_chunks(P, nsel > 0 ? nsel : (rows + kQBlock - 1) / kQBlock, F, &iters);
   *ml = (size_t)rup((int64_t)((size_t)P * nch * G * kHeadDimH * 4), 256);
   return nch == 1 ? 256 : *ml + (size_t)rup((int64_t)((size_t)P * nch * G * 2 * 4), 256);
 }

@@ -33,7 +33,7 @@ namespace arckv {
 namespace {
 constexpr int kAqW = 4;               // waves per workgroup
 constexpr int kAqSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
-constexpr int kAqStart = 4;           // cost of a workgroup beside its blocks, in blocks per wave
+constexpr int kAqStart = 6;           // cost of a workgroup beside its blocks, in blocks per wave
 constexpr int kAqTail = 32;           // tail rows per wave
 // Bytes of codes above which the values are read as a stream that the caches do not keep: the last-level cache's size.
 constexpr int64_t kAttendKept = (int64_t)256 << 20;
@@ -168,7 +168,7 @@ struct AttendQ {
   const bf16 *Kf, *Vf;
   const int32_t *length_f;
   float *part_o, *part_ml, *out;
-  int iters, tail_iters, nch; // blocks and tail units per wave of a chunk; chunks per pair
+  int iters, nch;             // units (blocks, 32 tail rows) per wave of a chunk; chunks per pair
 };
 
 // What a wave has in flight of a block of 64 tokens.  Keys as MFMA rows, where a contraction step pairs bytes
@@ -418,19 +418,19 @@ __global__ void __launch_bounds__(64 * kAqW, 3) k_attendq_partial(AttendQ a) {
                                                8 * (ks % 2));
   float m = -INFINITY, l = 0.0f;
   f32x4 o[8] = {};
-  {
-    const int len = clip_len(a.length, p, a.c.rows), first = ch * a.iters * kAqW;
-    int end = min(first + a.iters * kAqW, a.nsel);
-    if (!a.blocks) end = min(end, (len + kQBlock - 1) / kQBlock);
-    if (first + wave < end)
-      attend_blocks<FMT, BETA, STREAM>(a, p, first + wave, end, len, sB[BETA ? wave : 0], qf, sQ[wave], m, l, o);
-    else
-      put_queries(qf, sQ[wave]);
-  }
-  if (a.F) {
-    const int len = clip_len(a.length_f, p, a.F), first = ch * a.tail_iters * kAqW;
-    const int end = min(first + a.tail_iters * kAqW, (len + kAqTail - 1) / kAqTail);
-    if (first + wave < end) attend_tail<STREAM>(a, p, first + wave, end, len, sQ[wave], m, l, o);
+  // units: the blocks (or list entries), then the tail's 32-row pieces; this chunk's, wave by wave
+  const int first = ch * a.iters * kAqW + wave, end = ch * a.iters * kAqW + a.iters * kAqW;
+  const int len = clip_len(a.length, p, a.c.rows);
+  const int bend = min(end, a.blocks ? a.nsel : (len + kQBlock - 1) / kQBlock);
+  if (first < bend)
+    attend_blocks<FMT, BETA, STREAM>(a, p, first, bend, len, sB[BETA ? wave : 0], qf, sQ[wave], m, l, o);
+  else
+    put_queries(qf, sQ[wave]);
+  if (end > a.nsel) {
+    const int len_f = clip_len(a.length_f, p, a.F);
+    const int skip = first < a.nsel ? (a.nsel - first + kAqW - 1) / kAqW * kAqW : 0;   // this wave's blocks
+    const int tfirst = first + skip - a.nsel, tend = min(end - a.nsel, (len_f + kAqTail - 1) / kAqTail);
+    if (tfirst < tend) attend_tail<STREAM>(a, p, tfirst, tend, len_f, sQ[wave], m, l, o);
   }
   if (g == 0 && r < G) {
     sM[wave][r] = m;
@@ -491,34 +491,33 @@ __global__ void __launch_bounds__(kHeadDim) k_attendq_combine(AttendQ a) {
   a.out[((int64_t)p * a.G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
 }
 
-// Chunks per pair, and each wave's blocks and tail units of one.  Workgroups run kAqSlots at a time, so a call takes as
-// many rounds as they fill, of a workgroup's units and its start each; the number of chunks with the least sum is taken:
-// 512 pairs of 3277 + 256 rows 80 us as one chunk each (96 us as three), of 8192 to 16384 rows 272 us as three.
-int attendq_chunks(int P, int nsel, int F, int *iters, int *tail_iters) {
-  const int nb = (nsel + kAqW - 1) / kAqW, nt = ((F + kAqTail - 1) / kAqTail + kAqW - 1) / kAqW, most = max(nb, nt);
-  auto per = [](int n, int c) { return (n + c - 1) / c; };
-  int best = most;
-  if ((int64_t)P * most > kAqSlots) {
+// Chunks per pair, and the units (blocks and 32-row pieces of the tail) per wave of one.  Workgroups run kAqSlots at a
+// time, so a call takes as many rounds as they fill, of a workgroup's units and its start each; the number of chunks with
+// the least sum is taken: 512 pairs of 3277 + 256 rows 80 us as one chunk each (96 us as three), of 8192 to 16384 rows
+// 272 us as three.
+int attendq_chunks(int P, int nsel, int F, int *iters) {
+  const int n = (nsel + (F + kAqTail - 1) / kAqTail + kAqW - 1) / kAqW;   // a pair's units by fours
+  *iters = 1;
+  if ((int64_t)P * n > kAqSlots) {
     int64_t least = INT64_MAX;
-    for (int c = 1; c <= most && (int64_t)P * (c - 1) < 4 * kAqSlots; ++c) {
-      const int64_t rounds = ((int64_t)P * c + kAqSlots - 1) / kAqSlots, cost = rounds * (per(nb, c) + per(nt, c) + kAqStart);
+    for (int c = 1; c <= n && (int64_t)P * (c - 1) < 4 * kAqSlots; ++c) {
+      const int it = (n + c - 1) / c;
+      const int64_t cost = ((int64_t)P * c + kAqSlots - 1) / kAqSlots * (it + kAqStart);
       if (cost < least) {
         least = cost;
-        best = c;
+        *iters = it;
       }
     }
   }
-  *iters = per(nb, best);
-  *tail_iters = per(nt, best);
-  return best;
+  return (n + *iters - 1) / *iters;
 }
 
 hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const int32_t *blocks, int nsel, const void *Kf, const void *Vf,
                           const int32_t *length_f, float *part_o, float *part_ml, float *out, hipStream_t s) {
   AttendQ a{c, G, F, scale, (const bf16 *)Q, beta, length, blocks, blocks ? nsel : c.nblk, (const bf16 *)Kf,
-            (const bf16 *)Vf, length_f, part_o, part_ml, out, 0, 0, 0};
-  a.nch = attendq_chunks(c.P, a.nsel, F, &a.iters, &a.tail_iters);
+            (const bf16 *)Vf, length_f, part_o, part_ml, out, 0, 0};
+  a.nch = attendq_chunks(c.P, a.nsel, F, &a.iters);
   // pairs over y and z: a grid's y extent is limited
   const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
   const bool stream = (int64_t)c.P * a.nsel * kQBlock * 2 * kHeadDim > kAttendKept;

@@ -7,6 +7,8 @@
 // nearest, ties to even.  Powers of two make the division exact, so the codes
 // are the same however they are computed, a stored value (scale times code) is
 // exact in bf16, and writing a stored value again changes nothing.
+#include <type_traits>
+
 #include "qcode.hpp"
 
 namespace arckv {
@@ -211,87 +213,203 @@ hipError_t launch_qcache_read(int fmt, int dtype, const QCache &c, int first, in
 // s_b = max_g [ scale * kappa_b * sum_d max(q_gd lo_bd, q_gd hi_bd) ] (+ max beta of
 // the block's tokens): no logit of the block's stored keys exceeds it.  The
 // order of blocks decides what a step attends to, so it must not hang on the
-// rounding of a sum: the products of an 8-bit significand and a code are exact
-// in float32, and their sum is taken in float64, where it is exact for queries
-// whose channels span less than about 2^30.  Four lanes share a block, 32 channels each.
-template <int FMT>
+// rounding of a sum: the sums are exact, and rounded once to float32.
+//
+// The sum is (q+ . hi) + (q- . lo) with the positive and negative parts of q, a
+// product of matrices, and MFMA's float32 sums are exact if every product is a
+// whole number of units and their sum stays below 2^24 of them.  So a query row
+// enters as four planes of 8 bits each below its largest magnitude 2^E,
+//   q = sum_t D_t 2^(E - 8 (t + 1)), D_t whole, |D_t| < 256
+// (exact for channels down to 2^(E - 24); smaller ones lose what lies below
+// 2^(E - 32)), four query rows times four planes filling the 16 columns, and
+// codes as they are (int8: |c| <= 127, units of 1) or as nearest whole numbers
+// and the rests in units of 2^-9 (e4m3: both at most 448 and 256 units): at
+// most 448 * 255 * 128 < 2^24.  The planes' sums meet in float64.
+constexpr int kBsTile = 16;   // blocks per wave and step
+
+// max and sum over lanes of a 16-lane row by DPP moves of a double's halves
+template <int CTRL> __device__ inline double dpp(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)u, CTRL, 0xf, 0xf, true),
+                 hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+constexpr int kDppXor1 = 0xb1, kDppXor2 = 0x4e, kDppRor4 = 0x124, kDppRor8 = 0x128;
+// the larger; a NaN wins
+__device__ inline double nan_max(double a, double b) { return a > b || a != a ? a : b; }
+
+__device__ inline f32x4 mfma_f16(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight codes as fp16: whole numbers and, for e4m3, rests.
+template <int FMT> __device__ inline void code_parts(uint32_t w0, uint32_t w1, f16x8 &whole, f16x8 &rest) {
+  uint32_t out[4], low[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w = i ? w1 : w0;
+    if constexpr (FMT == ARCKV_INT8) {
+      // a byte u below fp16's exponent of 1024 is 1024 + u; with the code's sign bit flipped u is code + 128
+      const f16x2 off = {(f16)-1152.0f, (f16)-1152.0f};
+      const uint32_t u = w ^ 0x80808080u;
+      out[2 * i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off);
+      out[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f16x2 big = {(f16)1536.0f, (f16)1536.0f};   // fp16 steps by 1 here
+        const f16x2 x = __builtin_bit_cast(f16x2, h ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)
+                                                    : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+        const f16x2 n = (x + big) - big;
+        out[2 * i + h] = __builtin_bit_cast(uint32_t, n);
+        low[2 * i + h] = __builtin_bit_cast(uint32_t, x - n);
+      }
+    }
+  }
+  __builtin_memcpy(&whole, out, 16);
+  if constexpr (FMT == ARCKV_E4M3) __builtin_memcpy(&rest, low, 16);
+}
+
+// CT: tiles of 16 columns, four query rows each.  A wave takes tiles of 16 blocks; blockIdx.x strides over them.
+template <int FMT, int CT, bool BETA>
 __global__ void __launch_bounds__(256) k_block_scores(QCache c, int G, double scale, const bf16 *__restrict__ Q,
                                                       const float *__restrict__ beta,
                                                       const int32_t *__restrict__ length,
                                                       float *__restrict__ scores) {
-  __shared__ float sQ[16][4][36];   // a part's 32 channels, padded so that the four parts lie in different banks
-  const int tid = threadIdx.x, part = tid & 3;
-  const int b = blockIdx.x * 64 + (tid >> 2);
-  for (int p = blockIdx.y; p < c.P; p += gridDim.y) {
-    __syncthreads();
-    for (int i = tid; i < G * kHeadDim; i += 256)
-      sQ[i / kHeadDim][(i % kHeadDim) / 32][i % 32] = (float)Q[(int64_t)p * G * kHeadDim + i];
-    __syncthreads();
-    const int len = clip_len(length, p, c.rows);
-    if (b >= c.nblk) continue;
-    if (b * kQBlock >= len) {
-      if (part == 0) scores[(int64_t)p * c.nblk + b] = -INFINITY;
+  __shared__ __align__(16) f16 sD[2][16 * CT][kHeadDim + 8];   // planes of q+ and q-, row = column 4 g + t; padded for the banks
+  __shared__ int sE[4 * CT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = lane >> 4, r = lane & 15;
+  const int p = blockIdx.z * gridDim.y + blockIdx.y;
+  if (p >= c.P) return;
+  const int len = clip_len(length, p, c.rows);
+  // ---- the planes: 16 threads a query row, 8 channels each
+  if (tid < 64 * CT) {
+    const int g = tid >> 4, d = 8 * (tid & 15);
+    bf16x8 q = {};
+    if (g < G) q = *reinterpret_cast<const bf16x8 *>(Q + ((int64_t)p * G + g) * kHeadDim + d);
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint((float)q[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
+    const bool finite = amax < 0x7f800000u;
+    int E = 0;
+    if (finite && amax) E = __builtin_amdgcn_frexp_expf(__uint_as_float(amax));   // amax < 2^E
+    if ((tid & 15) == 0) sE[g] = E;
+    f16x8 plane[4][2];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float x = ldexpf((float)q[e], 8 - E);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float n = finite ? truncf(x) : __uint_as_float(0x7fc00000u);   // a non-finite query gives NaN scores
+        plane[t][0][e] = (f16)(n > 0.0f || n != n ? n : 0.0f);
+        plane[t][1][e] = (f16)(n < 0.0f ? n : 0.0f);
+        x = (x - n) * 256.0f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) *reinterpret_cast<f16x8 *>(&sD[s][4 * g + t][d]) = plane[t][s];
+  }
+  __syncthreads();
+  // weights of this lane's columns; a row that is not there never is the largest
+  double weight[CT], floor_[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int g = 4 * ct + (r >> 2);
+    weight[ct] = ldexp(1.0, sE[g] - 8 * ((r & 3) + 1));
+    floor_[ct] = g < G ? 0.0 : -INFINITY;
+  }
+  const int tiles = (c.nblk + kBsTile - 1) / kBsTile;
+  for (int tile = blockIdx.x * 4 + wave; tile < tiles; tile += gridDim.x * 4) {
+    const int b0 = tile * kBsTile;
+    if (b0 * kQBlock >= len) {
+      if (lane < kBsTile && b0 + lane < c.nblk) scores[(int64_t)p * c.nblk + b0 + lane] = -INFINITY;
       continue;
     }
-    const uint8_t *bd = c.bounds + ((int64_t)p * c.nblk + b) * 2 * kHeadDim + 32 * part;
-    float lo[32], hi[32];
+    const uint8_t *row = c.bounds + ((int64_t)p * c.nblk + min(b0 + r, c.nblk - 1)) * 2 * kHeadDim + 16 * kg;
+    uint4 lo[2], hi[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint4 l = *reinterpret_cast<const uint4 *>(bd + 16 * k), h = *reinterpret_cast<const uint4 *>(bd + kHeadDim + 16 * k);
-      const uint32_t lw[4] = {l.x, l.y, l.z, l.w}, hw[4] = {h.x, h.y, h.z, h.w};
+    for (int kk = 0; kk < 2; ++kk) {
+      lo[kk] = *reinterpret_cast<const uint4 *>(row + 64 * kk);
+      hi[kk] = *reinterpret_cast<const uint4 *>(row + kHeadDim + 64 * kk);
+    }
+    // this lane's output: block 4 kg + r of the tile (r < 4)
+    const int b = b0 + 4 * kg + (r & 3);
+    const bool there = b < c.nblk && b * kQBlock < len;
+    const double kscale = there ? scale * (double)c.Ks[(int64_t)p * c.nblk + b] : 0.0;
+    float top = -INFINITY;
+    if constexpr (BETA) {
+      // four lanes a block, 16 biases each
+      const int bb = b0 + (lane >> 2), j0 = bb * kQBlock + 16 * (lane & 3), j1 = min(j0 + 16, len);
+      for (int j = j0; j < j1; ++j) {
+        const float x = beta[(int64_t)p * c.rows + j];
+        top = x > top || x != x ? x : top;
+      }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float y[4], z[4];
-        QCode<FMT>::unpack4(lw[j], y);
-        QCode<FMT>::unpack4(hw[j], z);
+      for (int m = 1; m <= 2; m <<= 1) {
+        const float x = __shfl_xor(top, m, 64);
+        top = x > top || x != x ? x : top;
+      }
+      top = __shfl(top, 4 * (4 * kg + (r & 3)), 64);
+    }
+    f32x4 acc[CT][2] = {};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          lo[16 * k + 4 * j + e] = y[e];
-          hi[16 * k + 4 * j + e] = z[e];
-        }
+    for (int ks = 0; ks < 4; ++ks) {
+      // channels 64 kk + 16 kg + 8 h .. + 7, as the codes were read
+      const int kk = ks / 2, h = ks % 2, d = 64 * kk + 16 * kg + 8 * h;
+      f16x8 hn, hr, ln, lr;
+      code_parts<FMT>(h ? hi[kk].z : hi[kk].x, h ? hi[kk].w : hi[kk].y, hn, hr);
+      code_parts<FMT>(h ? lo[kk].z : lo[kk].x, h ? lo[kk].w : lo[kk].y, ln, lr);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const f16x8 qp = *reinterpret_cast<const f16x8 *>(&sD[0][16 * ct + r][d]),
+                    qn = *reinterpret_cast<const f16x8 *>(&sD[1][16 * ct + r][d]);
+        acc[ct][0] = mfma_f16(ln, qn, mfma_f16(hn, qp, acc[ct][0]));
+        if constexpr (FMT == ARCKV_E4M3) acc[ct][1] = mfma_f16(lr, qn, mfma_f16(hr, qp, acc[ct][1]));
       }
     }
-    double best = -INFINITY;
-    bool nan = false;
-    for (int g = 0; g < G; ++g) {
-      double sum = 0.0;
+    double best = 0.0;
 #pragma unroll
-      for (int d = 0; d < 32; ++d) {
-        const float q = sQ[g][part][d];
-        sum += (double)(q * (q >= 0.0f ? hi[d] : lo[d]));
+    for (int j = 0; j < 4; ++j) {   // blocks 4 kg + j
+      double m = -INFINITY;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        double x = (double)acc[ct][0][j];
+        if constexpr (FMT == ARCKV_E4M3) x += (double)acc[ct][1][j];
+        x *= weight[ct];
+        x += dpp<kDppXor1>(x);
+        x += dpp<kDppXor2>(x);
+        m = nan_max(m, x + floor_[ct]);
       }
-      sum += __shfl_xor(sum, 1, 64);
-      sum += __shfl_xor(sum, 2, 64);
-      nan |= sum != sum;
-      best = fmax(best, sum);
+      m = nan_max(m, dpp<kDppRor4>(m));
+      m = nan_max(m, dpp<kDppRor8>(m));
+      best = (r & 3) == j ? m : best;
     }
-    double score = best * (scale * (double)c.Ks[(int64_t)p * c.nblk + b]);
-    if (beta) {
-      const float *row = beta + (int64_t)p * c.rows + b * kQBlock;
-      float top = -INFINITY;
-      for (int j = part; j < min(kQBlock, len - b * kQBlock); j += 4) {
-        nan |= row[j] != row[j];
-        top = fmaxf(top, row[j]);
-      }
-      top = fmaxf(top, __shfl_xor(top, 1, 64));
-      top = fmaxf(top, __shfl_xor(top, 2, 64));
-      score = top == -INFINITY ? -INFINITY : score + (double)top;
-    }
-    int bad = nan;
-    bad |= __shfl_xor(bad, 1, 64);
-    bad |= __shfl_xor(bad, 2, 64);
-    if (part == 0) scores[(int64_t)p * c.nblk + b] = bad ? __uint_as_float(0x7fc00000u) : (float)score;
+    double score = best * kscale;
+    if constexpr (BETA) score = top == -INFINITY ? -INFINITY : score + (double)top;
+    if (r < 4 && b < c.nblk) scores[(int64_t)p * c.nblk + b] = there ? (float)score : -INFINITY;
   }
 }
 
 hipError_t launch_select_blocks(int fmt, const QCache &c, int G, double scale, const void *Q, const float *beta,
                                 const int32_t *length, int k, float *scores, int32_t *blocks, hipStream_t s) {
-  const dim3 grid((unsigned)((c.nblk + 63) / 64), (unsigned)min(c.P, 65535));
+  const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
+  const dim3 grid((unsigned)((c.nblk + 4 * kBsTile - 1) / (4 * kBsTile)), py, pz);
   auto go = [&](auto kern) {
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, c, G, scale, (const bf16 *)Q, beta, length, scores);
     return hipGetLastError();
   };
-  const hipError_t e = fmt == ARCKV_E4M3 ? go(k_block_scores<ARCKV_E4M3>) : go(k_block_scores<ARCKV_INT8>);
+  auto by_rows = [&](auto fm, auto bt) {
+    constexpr int FMT = decltype(fm)::value;
+    constexpr bool BETA = decltype(bt)::value;
+    return G <= 4 ? go(k_block_scores<FMT, 1, BETA>) : G <= 8 ? go(k_block_scores<FMT, 2, BETA>) : go(k_block_scores<FMT, 4, BETA>);
+  };
+  auto by_beta = [&](auto fm) { return beta ? by_rows(fm, std::true_type{}) : by_rows(fm, std::false_type{}); };
+  const hipError_t e = fmt == ARCKV_E4M3 ? by_beta(std::integral_constant<int, ARCKV_E4M3>{})
+                                         : by_beta(std::integral_constant<int, ARCKV_INT8>{});
   return e != hipSuccess ? e : launch_select(scores, c.P, c.nblk, k, blocks, s);
 }
 

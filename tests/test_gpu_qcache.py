@@ -418,8 +418,10 @@ def check_select(blocks, scores, Q, c, k, beta, length, s):
         got = np64(scores[p])
         fin = np.isfinite(want)
         assert np.array_equal(np.isfinite(got), fin) and np.array_equal(got[~fin], want[~fin])
-        # half a step of float32 and, for the float64 sum's own roundings, a little more
-        assert (np.abs(got[fin] - want[fin]) <= np.abs(want[fin]) * (U + 2.0 ** -40)).all()
+        # half a step of float32; for the float64 sums' own roundings a little more; what is cut off the 128 channels
+        reach = np.abs(np64(c.K_bounds[p])[fin]).max(axis=(1, 2)) * np64(c.K_scale[p])[fin]
+        cut = 128 * 2.0 ** -32 * 2 * np.abs(np64(Q[p])).max() * reach * s
+        assert (np.abs(got[fin] - want[fin]) <= np.abs(want[fin]) * (U + 2.0 ** -40) + cut).all()
         assert blocks[p].tolist() == sorted(oracle.select_topt(scores[p].cpu().numpy(), k).tolist())
 
 
@@ -436,6 +438,35 @@ def test_select_blocks(fmt, P, G, R, k):
     for b in (None, beta):
         blocks, scores = A().select_blocks(Q, c, k, b)
         check_select(blocks, scores, Q, c, k, b, None, float(S))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_select_blocks_wide_queries(fmt):
+    """Channels that span 2^20 and more, of both signs, rows of zeros and of the smallest numbers: the sums stay exact for
+    channels down to 2^-24 of the largest, so blocks that differ in their smallest channels alone keep their order."""
+    g = np.random.default_rng(35)
+    P, R, G = 3, 1500, 8
+    c = filled(g, P, R, fmt)
+    e = torch.from_numpy(g.uniform(-22, 0, (P, G, 128)).astype(np.float32)).cuda().exp2()
+    Q = (rows(g, P, G, 128).sign() * e).to(torch.bfloat16)
+    Q[1, 2:] = 0
+    Q[2] *= 2.0 ** -120
+    blocks, scores = A().select_blocks(Q, c, 6)
+    check_select(blocks, scores, Q, c, 6, None, None, float(S))
+    Q[0, 3, 7] = math.nan
+    Q[1, 1, 9] = math.inf
+    _, bad = A().select_blocks(Q, c, 6)
+    assert bad[:2].isnan().all() and torch.equal(bad[2], scores[2])
+    # blocks alike but for one code in a channel that the query weighs 2^-22 as much as the others
+    K = rows(g, 1, 1, 128).repeat(1, 640, 1)
+    K[0, 5 * 64:6 * 64, 3] += 0.25
+    t = make_cache(1, 640, fmt)
+    A().qcache_write(t, K, K)
+    q = torch.ones(1, 1, 128, device="cuda")
+    q[0, 0, 3] = 2.0 ** -22
+    q = q.to(torch.bfloat16)
+    blocks, scores = A().select_blocks(q, t, 1)
+    check_select(blocks, scores, q, t, 1, None, None, float(S))
 
 
 def test_select_blocks_ragged_masked_and_tied():

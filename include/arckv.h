@@ -460,7 +460,8 @@ arckv_status arckv_select_blocks(const arckv_qcache *c, int32_t G, float scale, 
  *   length_f [P] device array of rows held in K_f, V_f (clipped to [0, F]), or NULL: F.
  *   out      [P][G][128] float32; zeros for a pair without any row to attend to.
  * All tensors 16-byte aligned (per-pair int32 and float32 arrays by element).
- * Workspace: arckv_attend_qcache_workspace_size bytes.  Reads every code once. */
+ * Workspace: arckv_attend_qcache_workspace_size bytes; 0 where a pair's rows are one
+ * workgroup's work, ws may then be NULL.  Reads every code once. */
 arckv_status arckv_attend_qcache_workspace_size(int32_t P, int32_t rows, int32_t G, int32_t nsel, int32_t F,
                                                 size_t *bytes);
 arckv_status arckv_attend_qcache(const arckv_qcache *c, int32_t G, int32_t nsel, int32_t F, float scale, const void *Q,

@@ -483,27 +483,29 @@ def _qptr(x: Optional[torch.Tensor], shape, dtype: torch.dtype, device: int, wha
     """Pointer of a tensor that has to have this shape and type and live on the current device."""
     if x is None:
         return None
+    # one chain: a decode call checks up to a dozen tensors, 0.6 us each
+    if x.dtype is dtype and x.shape == shape and x.is_contiguous() and x.get_device() == device:
+        return x.data_ptr()
     if x.dtype != dtype:
         raise TypeError(f"{what}: expected {dtype}, got {x.dtype}")
     if x.shape != shape:
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
     if x.get_device() != device:
         raise ValueError(f"{what}: tensors must live on the current GPU")
-    if not x.is_contiguous():
-        raise ValueError(f"{what}: tensors must be contiguous")
-    return x.data_ptr()
+    raise ValueError(f"{what}: tensors must be contiguous")
 
 
 def _qcache(c) -> tuple:
     """(struct, P, rows, current device) of a cache tuple."""
     K, V, Ks, Vs, bounds = c
-    P, rows, d = K.shape
-    dev = torch.cuda.current_device()
+    shape, dtype, dev = K.shape, K.dtype, torch.cuda.current_device()
+    P, rows, d = shape
     n = -(-rows // QBLOCK)
-    return QCacheStruct(P, rows, d, _qformat(K.dtype), _qptr(K, K.shape, K.dtype, dev, "K"),
-                        _qptr(V, K.shape, K.dtype, dev, "V"), _qptr(Ks, (P, n), torch.float32, dev, "K_scale"),
-                        _qptr(Vs, (P, n), torch.float32, dev, "V_scale"),
-                        _qptr(bounds, (P, n, 2, d), K.dtype, dev, "K_bounds")), P, rows, dev
+    scales = (P, n)
+    return QCacheStruct(P, rows, d, _qformat(dtype), _qptr(K, shape, dtype, dev, "K"),
+                        _qptr(V, shape, dtype, dev, "V"), _qptr(Ks, scales, torch.float32, dev, "K_scale"),
+                        _qptr(Vs, scales, torch.float32, dev, "V_scale"),
+                        _qptr(bounds, (P, n, 2, d), dtype, dev, "K_bounds")), P, rows, dev
 
 
 def qcache_write(cache, K, V, start=None, count=None) -> None:
@@ -514,7 +516,8 @@ def qcache_write(cache, K, V, start=None, count=None) -> None:
     _check(lib().arckv_qcache_write(ctypes.byref(st), n, _dtype_code(K.dtype), _qptr(K, (P, n, 128), K.dtype, dev, "K"),
                                     _qptr(V, (P, n, 128), K.dtype, dev, "V"),
                                     _qptr(start, (P,), torch.int32, dev, "start"),
-                                    _qptr(count, (P,), torch.int32, dev, "count"), _stream()), "arckv_qcache_write")
+                                    _qptr(count, (P,), torch.int32, dev, "count"),
+                                    torch._C._cuda_getCurrentRawStream(dev)), "arckv_qcache_write")
 
 
 def qcache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bfloat16, length=None):
@@ -525,7 +528,8 @@ def qcache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bflo
     code = _dtype_code(dtype)
     K, V = torch.empty(2, P, max(n, 0), 128, dtype=dtype, device=cache[0].device)
     _check(lib().arckv_qcache_read(ctypes.byref(st), int(first), n, code, _qptr(length, (P,), torch.int32, dev, "length"),
-                                   K.data_ptr(), V.data_ptr(), _stream()), "arckv_qcache_read")
+                                   K.data_ptr(), V.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
+           "arckv_qcache_read")
     return K, V
 
 
@@ -540,7 +544,8 @@ def select_blocks(Q, cache, k: int, beta=None, length=None, scale=None):
                                      _qptr(Q, (P, G, 128), torch.bfloat16, dev, "Q"),
                                      _qptr(beta, (P, rows), torch.float32, dev, "beta"),
                                      _qptr(length, (P,), torch.int32, dev, "length"), int(k), scores.data_ptr(),
-                                     blocks.data_ptr(), _stream()), "arckv_select_blocks")
+                                     blocks.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
+           "arckv_select_blocks")
     return blocks, scores
 
 
@@ -563,24 +568,32 @@ def attend_qcache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f
     nsel = blocks.shape[1] if blocks is not None else 0
     if blocks is not None and nsel == 0:
         raise ValueError("blocks: an empty list")
+    row = (P,)
     if out is None:
         out = torch.empty(P, G, 128, dtype=torch.float32, device=Q.device)
+        optr = out.data_ptr()
+    else:
+        optr = _qptr(out, (P, G, 128), torch.float32, dev, "out")
     if ws is None:
-        nbytes = attend_qcache_workspace_size(P, rows, G, nsel, F)
-        ws = _workspace(nbytes, Q.device)
+        nbytes = ctypes.c_size_t()
+        _check(lib().arckv_attend_qcache_workspace_size(P, rows, G, nsel, F, ctypes.byref(nbytes)),
+               "arckv_attend_qcache_workspace_size")
+        nbytes = nbytes.value
+        # torch's device allocations are 512-byte aligned
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
+        wptr = ws.data_ptr() if nbytes else None
     else:
         nbytes = ws.numel()
+        wptr = _qptr(ws, ws.shape, torch.uint8, dev, "ws")
     _check(lib().arckv_attend_qcache(ctypes.byref(st), G, nsel, F, float(scale) if scale else 0.0,
                                      _qptr(Q, (P, G, 128), torch.bfloat16, dev, "Q"),
                                      _qptr(beta, (P, rows), torch.float32, dev, "beta"),
-                                     _qptr(length, (P,), torch.int32, dev, "length"),
+                                     _qptr(length, row, torch.int32, dev, "length"),
                                      _qptr(blocks, (P, nsel), torch.int32, dev, "blocks"),
                                      _qptr(K_f, (P, F, 128), torch.bfloat16, dev, "K_f"),
                                      _qptr(V_f, (P, F, 128), torch.bfloat16, dev, "V_f"),
-                                     _qptr(length_f, (P,), torch.int32, dev, "length_f"),
-                                     _qptr(out, (P, G, 128), torch.float32, dev, "out"),
-                                     _qptr(ws, ws.shape, torch.uint8, dev, "ws"), nbytes, _stream()),
-           "arckv_attend_qcache")
+                                     _qptr(length_f, row, torch.int32, dev, "length_f"), optr, wptr, nbytes,
+                                     torch._C._cuda_getCurrentRawStream(dev)), "arckv_attend_qcache")
     return out
 
 

@@ -1067,7 +1067,7 @@ static size_t attend_qcache_ws_bytes(int32_t P, int32_t rows, int32_t G, int32_t
   int iters;
   const size_t nch = (size_t)attendq_chunks(P, nsel > 0 ? nsel : (rows + kQBlock - 1) / kQBlock, F, &iters);
   *ml = (size_t)rup((int64_t)((size_t)P * nch * G * kHeadDimH * 4), 256);
-  return nch == 1 ? 256 : *ml + (size_t)rup((int64_t)((size_t)P * nch * G * 2 * 4), 256);
+  return nch == 1 ? 0 : *ml + (size_t)rup((int64_t)((size_t)P * nch * G * 2 * 4), 256);
 }
 
 arckv_status arckv_attend_qcache_workspace_size(int32_t P, int32_t rows, int32_t G, int32_t nsel, int32_t F,
@@ -1092,7 +1092,7 @@ arckv_status arckv_attend_qcache(const arckv_qcache *c, int32_t G, int32_t nsel,
     return ARCKV_ERR_INVALID_ARG;
   size_t ml;
   const size_t need = attend_qcache_ws_bytes(c->P, c->rows, G, nsel, F, &ml);
-  if (!ws || !aligned(ws, 256) || ws_bytes < need) return ARCKV_ERR_WORKSPACE;
+  if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return ARCKV_ERR_WORKSPACE;
   const float s = scale > 0.0f ? scale : 1.0f / sqrtf((float)kHeadDimH);
   STAGE(ST_ATTEND_QCACHE,
         launch_attendq(c->format, make_qcache(c), G, F, s, Q, beta, length, blocks, nsel, F > 0 ? K_f : nullptr,

@@ -32,6 +32,7 @@ namespace arckv {
 
 namespace {
 constexpr int kAqW = 4;               // waves per workgroup
+constexpr int kAqWide = 16;           // of one that takes a whole pair of a small call, one unit per wave
 constexpr int kAqSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
 constexpr int kAqStart = 6;           // cost of a workgroup beside its blocks, in blocks per wave
 constexpr int kAqTail = 32;           // tail rows per wave
@@ -88,18 +89,15 @@ template <> struct Operand<ARCKV_INT8> {
   }
 };
 
-// Probabilities of 8 keys, times 2^kPShift, as two fp16 terms: 22 bits of the large ones, and 2^-39 of the block's
-// largest where they are small.
+// Probabilities, times 2^kPShift, as two fp16 terms: 22 bits of the large ones, and 2^-39 of the block's largest where
+// they are small.
 constexpr float kPShift = 15.0f;
-__device__ inline void split_p_f16(const float *p, Frag &h, Frag &l) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const f32x2 x = {p[2 * k], p[2 * k + 1]};
-    const f16x2 hi = __builtin_convertvector(x, f16x2);
-    const f32x2 rest = {x[0] - (float)hi[0], x[1] - (float)hi[1]};
-    h.w[k] = __builtin_bit_cast(uint32_t, hi);
-    l.w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, f16x2));
-  }
+__device__ inline void split_p_f16(float p0, float p1, uint32_t &h, uint32_t &l) {
+  const f32x2 x = {p0, p1};
+  const f16x2 hi = __builtin_convertvector(x, f16x2);
+  const f32x2 rest = {x[0] - (float)hi[0], x[1] - (float)hi[1]};
+  h = __builtin_bit_cast(uint32_t, hi);
+  l = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, f16x2));
 }
 
 // Probabilities of 8 keys as three bf16 terms (truncated, so all of one sign) that
@@ -122,15 +120,32 @@ __device__ inline void split_p(const float *p, Frag &h, Frag &m, Frag &l) {
   }
 }
 
-// One step of a running softmax per query (columns r, keys over the lane's N and over g): turns the logits into
-// probabilities times 2^kPShift relative to the new maximum, takes them up in m and l, and returns what the earlier sums
-// have to be multiplied by.  -inf marks keys left out; any: whether there is one that is not.
-template <int N> __device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any) {
+// Reductions over the four 16-lane rows (g) of a wave, every lane with the result.
+template <typename F> __device__ inline float over_rows(float x, F f) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+// The word that lane r + FROM (mod 16) of the lane's row holds.
+template <int FROM> __device__ inline uint32_t from_lane(uint32_t x) {
+  return __builtin_amdgcn_update_dpp(0u, x, 0x120 + (16 - FROM), 0xf, 0xf, true);   // rotate right by 16 - FROM
+}
+template <int FROM> __device__ inline float from_lane(float x) { return __uint_as_float(from_lane<FROM>(__float_as_uint(x))); }
+
+// One step of a running softmax per query: turns the lane's N logits into probabilities times 2^kPShift relative to the
+// new maximum, takes them up in m and l, and returns what the earlier sums have to be multiplied by.  A query's logits lie
+// in the lanes of its column r of the four rows, and, PARTS > 1, of the columns r + 16 / PARTS, ....  -inf marks keys left
+// out; any: whether there is one that is not.
+template <int N, int PARTS> __device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any) {
+  auto larger = [](float x, float y) { return fmaxf(x, y); };
+  auto plus = [](float x, float y) { return x + y; };
   float top = sv[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, sv[i]);
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  if constexpr (PARTS == 4) top = fmaxf(top, from_lane<4>(top));
+  if constexpr (PARTS >= 2) top = fmaxf(top, from_lane<8>(top));
+  top = over_rows(top, larger);
   any = top != -INFINITY;
   top = fmaxf(top, m);
   const float ref = top == -INFINITY ? 0.0f : top;
@@ -141,8 +156,9 @@ template <int N> __device__ inline float softmax_step(float (&sv)[N], float &m, 
     sv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i] - ref, 1.44269504f, kPShift));
     sum += sv[i];
   }
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
+  if constexpr (PARTS == 4) sum += from_lane<4>(sum);
+  if constexpr (PARTS >= 2) sum += from_lane<8>(sum);
+  sum = over_rows(sum, plus);
   m = top;
   l = fmaf(l, keep, sum);
   return keep;
@@ -215,8 +231,8 @@ __device__ inline void put_queries(const bf16x8 (&qf)[4], bf16x8 *s_q) {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The blocks first, first + kAqW, ... below end of the list (or of the cache), a wave's share of a chunk.
-template <int FMT, bool BETA, bool STREAM>
+// The blocks first, first + W, ... below end of the list (or of the cache), a wave's share of a chunk.
+template <int W, int FMT, int GP, bool BETA, bool STREAM>
 __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end, int len, float *s_bias,
                                      const bf16x8 (&qf0)[4], bf16x8 *s_q, float &m, float &l, f32x4 (&o)[8]) {
   constexpr int NTV = STREAM ? 2 : 0;
@@ -238,31 +254,17 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
   load_values<NTV>(a, pb + b, pr + (int64_t)b * kQBlock, live, v);
   __builtin_amdgcn_sched_barrier(0);
   put_queries(qf0, s_q);
-  for (int idx = first; idx < end; idx += kAqW) {
+  for (int idx = first; idx < end; idx += W) {
     int nb, nlive;
-    block_at(idx + kAqW, nb, nlive);
-    float bv[16];
-    if constexpr (BETA) {
-      // one load per lane, spread to the lanes of a key's logits through LDS that only this wave uses
-      s_bias[lane] = lane < live ? k.bias : -INFINITY;
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const float4 x = *reinterpret_cast<const float4 *>(s_bias + 16 * kt + 4 * g);
-        bv[4 * kt] = x.x;
-        bv[4 * kt + 1] = x.y;
-        bv[4 * kt + 2] = x.z;
-        bv[4 * kt + 3] = x.w;
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-    // ---- logits: lane (g, r) holds keys 16 kt + 4 g + j (j < 4) for query r
+    block_at(idx + W, nb, nlive);
+    // ---- logits: keys 16 kt + 4 g + j (j < 4) of query r % GP, all four kt in every lane; the columns beyond the GP
+    // queries hold them again, and each of the 16 / GP copies goes on with its own share of the keys
+    constexpr int PARTS = 16 / GP, N = 16 / PARTS;
+    const int part = (lane & 15) / GP;
     bf16x8 qf[4];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) qf[ks] = s_q[ks * 64 + lane];
-    float sv[16];
-    const float kscale = k.scale * a.scale;
-    uint32_t masked = 0;
+    f32x4 dots[4];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -274,33 +276,84 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
         Operand<FMT>::bf16x4(c[2 * (ks % 2) + 1], f.w[2], f.w[3]);
         acc = mfma16(f.v, qf[ks], acc);
       }
+      dots[kt] = acc;
+    }
+    const float kscale = k.scale * a.scale;
+    float sv[N];
+    uint64_t hidden = 0;   // tokens in use with a bias of -inf, a bit each
+    if constexpr (BETA) {
+      // one bias per lane, spread to the lanes of a key's logits through LDS that only this wave uses
+      const float bias = lane < live ? k.bias : -INFINITY;
+      hidden = __ballot(lane < live && bias == -INFINITY);
+      s_bias[lane] = bias;
+      __builtin_amdgcn_wave_barrier();
+    }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 4 * kt + j;
-        if constexpr (BETA) {
-          const bool held = bv[i] != -INFINITY;
-          sv[i] = held ? fmaf(kscale, acc[j], bv[i]) : -INFINITY;
-          masked |= held ? 0u : 1u << i;
-        } else {
-          sv[i] = 16 * kt + 4 * g + j < live ? kscale * acc[j] : -INFINITY;
+    for (int t = 0; t < N / 4; ++t) {
+      const int key0 = 16 * (part * (N / 4) + t) + 4 * g;
+      f32x4 d = dots[t];
+#pragma unroll
+      for (int s = 1; s < PARTS; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[j] = part == s ? dots[s * (N / 4) + t][j] : d[j];
+      if constexpr (BETA) {
+        const float4 x = *reinterpret_cast<const float4 *>(s_bias + key0);
+        const float bv[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sv[4 * t + j] = bv[j] != -INFINITY ? fmaf(kscale, d[j], bv[j]) : -INFINITY;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sv[4 * t + j] = key0 + j < live ? kscale * d[j] : -INFINITY;
+      }
+    }
+    if constexpr (BETA) __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (W != kAqWide) load_keys<BETA>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
+    __builtin_amdgcn_sched_barrier(0);
+    bool any;
+    const float keep = softmax_step<N, PARTS>(sv, m, l, any);
+    if constexpr (BETA && FMT == ARCKV_E4M3) {
+      // the probability of a token left out is zero, but zero times a NaN code is not (int8 has none)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const uint32_t keeps = ~((uint32_t)(hidden >> 16 * t) >> 4 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t mask = (uint32_t)((int32_t)(keeps << (31 - j)) >> 31);
+          v.c[4 * t + j][0] &= mask;
+          v.c[4 * t + j][1] &= mask;
         }
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    load_keys<BETA>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
-    __builtin_amdgcn_sched_barrier(0);
-    bool any;
-    const float keep = softmax_step(sv, m, l, any);
-    if constexpr (BETA) {
+    // ---- (P V)^T: the probabilities of column r, query r, are the B operand with the lane's keys as contraction slots, and
+    // its values row r of eight A operands, one per dim 8 r + e: the sums of query r end up with its maximum
+    Frag ph[2], pl[2];   // of tokens 0..31 and 32..63; lane r collects the shares from the copies of its column
+    {
+      uint32_t h[N / 2], lo[N / 2];
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (masked >> i & 1) v.c[i] = u32x2{0u, 0u};   // its probability is zero, but zero times a NaN code is not
+      for (int i = 0; i < N / 2; ++i) split_p_f16(sv[2 * i], sv[2 * i + 1], h[i], lo[i]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (PARTS == 4) {
+          ph[0].w[i] = h[i];
+          pl[0].w[i] = lo[i];
+          ph[0].w[2 + i] = from_lane<4>(h[i]);
+          pl[0].w[2 + i] = from_lane<4>(lo[i]);
+          ph[1].w[i] = from_lane<8>(h[i]);
+          pl[1].w[i] = from_lane<8>(lo[i]);
+          ph[1].w[2 + i] = from_lane<12>(h[i]);
+          pl[1].w[2 + i] = from_lane<12>(lo[i]);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            ph[0].w[2 * u + i] = h[2 * u + i];
+            pl[0].w[2 * u + i] = lo[2 * u + i];
+            ph[1].w[2 * u + i] = PARTS == 2 ? from_lane<8>(h[2 * u + i]) : h[(4 + 2 * u + i) % (N / 2)];
+            pl[1].w[2 * u + i] = PARTS == 2 ? from_lane<8>(lo[2 * u + i]) : lo[(4 + 2 * u + i) % (N / 2)];
+          }
+        }
+      }
     }
-    // ---- (P V)^T: the lane's probabilities are column r of the B operand with its keys as contraction slots, and its
-    // values row r of eight A operands, one per dim 8 r + e: the sums of query r end up with its maximum
-    Frag ph[2], pl[2];
-    split_p_f16(sv, ph[0], pl[0]);
-    split_p_f16(sv + 8, ph[1], pl[1]);
     const float vscale = any ? v.scale : 0.0f;   // of a block that is left out whole it may be NaN
 #pragma unroll
     for (int dd = 0; dd < 2; ++dd) {
@@ -324,6 +377,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
         for (int j = 0; j < 4; ++j) o[4 * dd + e][j] = fmaf(vscale, acc[e][j], o[4 * dd + e][j] * keep);
     }
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (W == kAqWide) return;   // its only block
     load_values<NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, v);
     __builtin_amdgcn_sched_barrier(0);
     b = nb;
@@ -351,8 +405,8 @@ template <int NT> __device__ inline void load_tail_values(const AttendQ &a, int6
     v[i] = __builtin_amdgcn_raw_buffer_load_b128(vb, at + 2 * kHeadDim * (i % 4), 32 * kHeadDim * (i / 4), NT);
 }
 
-// The tail's units of 32 rows first, first + kAqW, ... below end, a wave's share of a chunk.
-template <bool STREAM>
+// The tail's units of 32 rows first, first + W, ... below end, a wave's share of a chunk.
+template <int W, bool STREAM>
 __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, int len, const bf16x8 *s_q, float &m,
                                    float &l, f32x4 (&o)[8]) {
   constexpr int NTV = STREAM ? 2 : 0;
@@ -363,9 +417,9 @@ __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, 
   u32x4 k[2][4], v[8];
   load_tail_keys(a, pr + first * kAqTail, live, k);
   load_tail_values<NTV>(a, pr + first * kAqTail, live, v);
-  for (int idx = first; idx < end; idx += kAqW) {
-    const int nlive = live_at(idx + kAqW);
-    const int64_t next = pr + (idx + kAqW) * kAqTail;
+  for (int idx = first; idx < end; idx += W) {
+    const int nlive = live_at(idx + W);
+    const int64_t next = pr + (idx + W) * kAqTail;
     float sv[8];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -376,10 +430,10 @@ __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, 
       for (int j = 0; j < 4; ++j) sv[4 * kt + j] = 16 * kt + 4 * g + j < live ? a.scale * acc[j] : -INFINITY;
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_tail_keys(a, next, nlive, k);
+    if constexpr (W != kAqWide) load_tail_keys(a, next, nlive, k);
     __builtin_amdgcn_sched_barrier(0);
     bool any;
-    const float keep = softmax_step(sv, m, l, any);
+    const float keep = softmax_step<8, 1>(sv, m, l, any);
     Frag ph, pm, pl;
     split_p(sv, ph, pm, pl);
 #pragma unroll
@@ -395,42 +449,47 @@ __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, 
       for (int j = 0; j < 4; ++j) o[e][j] = fmaf(o[e][j], keep, fabsf(lead[j]) < INFINITY ? lead[j] + rest[j] : lead[j]);
     }
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (W == kAqWide) return;
     load_tail_values<NTV>(a, next, nlive, v);
     __builtin_amdgcn_sched_barrier(0);
     live = nlive;
   }
 }
 
-// GP: the query rows that the LDS has room for, G <= GP <= 16.
-template <int FMT, int GP, bool BETA, bool STREAM>
-__global__ void __launch_bounds__(64 * kAqW, 3) k_attendq_partial(AttendQ a) {
-  __shared__ __align__(16) float sO[kAqW][GP][kHeadDim];
-  __shared__ float sM[kAqW][GP], sL[kAqW][GP];
-  __shared__ bf16x8 sQ[kAqW][4 * 64];   // each wave's query operands, [step][lane]
-  __shared__ __align__(16) float sB[BETA ? kAqW : 1][kQBlock];
+// GP: the query rows that LDS and operands have room for, G <= GP <= 16.
+template <int W, int FMT, int GP, bool BETA, bool STREAM>
+__global__ void __launch_bounds__(64 * W, W == kAqW ? 3 : 4) k_attendq_partial(AttendQ a) {
+  // a wave's query operands, [step][lane], and in their place its sums once they are complete
+  union Own {
+    bf16x8 q[4 * 64];
+    float o[GP][kHeadDim];
+  };
+  __shared__ __align__(16) Own sOwn[W];
+  __shared__ float sM[W][GP], sL[W][GP];
+  __shared__ __align__(16) float sB[BETA ? W : 1][kQBlock];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
   const int ch = blockIdx.x, p = blockIdx.z * gridDim.y + blockIdx.y, G = a.G;
   if (p >= a.c.P) return;
   bf16x8 qf[4];
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks)
-    qf[ks] = *reinterpret_cast<const bf16x8 *>(a.Q + ((int64_t)p * G + min(r, G - 1)) * kHeadDim + 64 * (ks / 2) + 16 * g +
+    qf[ks] = *reinterpret_cast<const bf16x8 *>(a.Q + ((int64_t)p * G + min(r % GP, G - 1)) * kHeadDim + 64 * (ks / 2) + 16 * g +
                                                8 * (ks % 2));
   float m = -INFINITY, l = 0.0f;
   f32x4 o[8] = {};
   // units: the blocks (or list entries), then the tail's 32-row pieces; this chunk's, wave by wave
-  const int first = ch * a.iters * kAqW + wave, end = ch * a.iters * kAqW + a.iters * kAqW;
+  const int first = ch * a.iters * W + wave, end = ch * a.iters * W + a.iters * W;
   const int len = clip_len(a.length, p, a.c.rows);
   const int bend = min(end, a.blocks ? a.nsel : (len + kQBlock - 1) / kQBlock);
   if (first < bend)
-    attend_blocks<FMT, BETA, STREAM>(a, p, first, bend, len, sB[BETA ? wave : 0], qf, sQ[wave], m, l, o);
+    attend_blocks<W, FMT, GP, BETA, STREAM>(a, p, first, bend, len, sB[BETA ? wave : 0], qf, sOwn[wave].q, m, l, o);
   else
-    put_queries(qf, sQ[wave]);
+    put_queries(qf, sOwn[wave].q);
   if (end > a.nsel) {
     const int len_f = clip_len(a.length_f, p, a.F);
-    const int skip = first < a.nsel ? (a.nsel - first + kAqW - 1) / kAqW * kAqW : 0;   // this wave's blocks
+    const int skip = first < a.nsel ? (a.nsel - first + W - 1) / W * W : 0;   // this wave's blocks
     const int tfirst = first + skip - a.nsel, tend = min(end - a.nsel, (len_f + kAqTail - 1) / kAqTail);
-    if (tfirst < tend) attend_tail<STREAM>(a, p, tfirst, tend, len_f, sQ[wave], m, l, o);
+    if (tfirst < tend) attend_tail<W, STREAM>(a, p, tfirst, tend, len_f, sOwn[wave].q, m, l, o);
   }
   if (g == 0 && r < G) {
     sM[wave][r] = m;
@@ -439,23 +498,23 @@ __global__ void __launch_bounds__(64 * kAqW, 3) k_attendq_partial(AttendQ a) {
   if (r < G)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      float *to = &sO[wave][r][8 * (4 * g + j)];
+      float *to = &sOwn[wave].o[r][8 * (4 * g + j)];
       *reinterpret_cast<float4 *>(to) = make_float4(o[0][j], o[1][j], o[2][j], o[3][j]);
       *reinterpret_cast<float4 *>(to + 4) = make_float4(o[4][j], o[5][j], o[6][j], o[7][j]);
     }
   __syncthreads();
   // one partial (max, sum, o) per query for the chunk; the result itself where there is one chunk
-  for (int idx = tid; idx < G * kHeadDim; idx += 64 * kAqW) {
+  for (int idx = tid; idx < G * kHeadDim; idx += 64 * W) {
     const int q = idx / kHeadDim, dim = idx % kHeadDim;
     float M = sM[0][q];
 #pragma unroll
-    for (int w = 1; w < kAqW; ++w) M = fmaxf(M, sM[w][q]);
+    for (int w = 1; w < W; ++w) M = fmaxf(M, sM[w][q]);
+    const float ref = M == -INFINITY ? 0.0f : M;
     float acc = 0.0f, lsum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kAqW; ++w) {
-      if (sM[w][q] == -INFINITY) continue;   // no key in use; its o may be zero times a NaN scale
-      const float f = __expf(sM[w][q] - M);
-      acc = fmaf(f, sO[w][q][dim], acc);
+    for (int w = 0; w < W; ++w) {
+      const float f = __expf(sM[w][q] - ref);   // a wave without a key in use: zero, as its sums are
+      acc = fmaf(f, sOwn[w].o[q][dim], acc);
       lsum = fmaf(f, sL[w][q], lsum);
     }
     if (a.nch == 1) {
@@ -491,12 +550,23 @@ __global__ void __launch_bounds__(kHeadDim) k_attendq_combine(AttendQ a) {
   a.out[((int64_t)p * a.G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
 }
 
+// Whether a call is small: one wide workgroup per pair takes its units in one step, and no second launch joins what it
+// leaves: 8 pairs of 819 + 37 rows @@.
+static bool attendq_small(int P, int nsel, int F) {
+  return P <= 256 && nsel + (F + kAqTail - 1) / kAqTail <= kAqWide;
+}
+
 // Chunks per pair, and the units (blocks and 32-row pieces of the tail) per wave of one.  Workgroups run kAqSlots at a
 // time, so a call takes as many rounds as they fill, of a workgroup's units and its start each; the number of chunks with
 // the least sum is taken: 512 pairs of 3277 + 256 rows 80 us as one chunk each (96 us as three), of 8192 to 16384 rows
 // 272 us as three.
 int attendq_chunks(int P, int nsel, int F, int *iters) {
-  const int n = (nsel + (F + kAqTail - 1) / kAqTail + kAqW - 1) / kAqW;   // a pair's units by fours
+  const int units = nsel + (F + kAqTail - 1) / kAqTail;
+  if (attendq_small(P, nsel, F)) {
+    *iters = 1;
+    return 1;
+  }
+  const int n = (units + kAqW - 1) / kAqW;
   *iters = 1;
   if ((int64_t)P * n > kAqSlots) {
     int64_t least = INT64_MAX;
@@ -521,14 +591,16 @@ hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, c
   // pairs over y and z: a grid's y extent is limited
   const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
   const bool stream = (int64_t)c.P * a.nsel * kQBlock * 2 * kHeadDim > kAttendKept;
+  const bool small = attendq_small(c.P, a.nsel, F);
   auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py, pz), dim3(64 * kAqW), 0, s, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py, pz), dim3(64 * (small ? kAqWide : kAqW)), 0, s, a);
     return hipGetLastError();
   };
   auto by_stream = [&](auto fm, auto gp, auto bt) {
     constexpr int FMT = decltype(fm)::value, GP = decltype(gp)::value;
     constexpr bool BETA = decltype(bt)::value;
-    return stream ? go(k_attendq_partial<FMT, GP, BETA, true>) : go(k_attendq_partial<FMT, GP, BETA, false>);
+    if (small) return go(k_attendq_partial<kAqWide, FMT, GP, BETA, false>);
+    return stream ? go(k_attendq_partial<kAqW, FMT, GP, BETA, true>) : go(k_attendq_partial<kAqW, FMT, GP, BETA, false>);
   };
   auto by_beta = [&](auto fm, auto gp) {
     return beta ? by_stream(fm, gp, std::true_type{}) : by_stream(fm, gp, std::false_type{});

@@ -146,16 +146,17 @@ def test_attend_qcache_refuses():
                      (dict(blocks=FAKE), A.ERR_INVALID_ARG), (dict(F=2), A.ERR_INVALID_ARG),
                      (dict(F=2, K_f=ODD), A.ERR_INVALID_ARG), (dict(scale=math.inf), A.ERR_INVALID_ARG),
                      (dict(Q=ODD), A.ERR_INVALID_ARG), (dict(out=None), A.ERR_INVALID_ARG),
-                     (dict(beta=ODD), A.ERR_INVALID_ARG), (dict(ws=None), A.ERR_WORKSPACE),
-                     (dict(ws=ODD), A.ERR_WORKSPACE), (dict(c=cache(rows=100000), n=1000), A.ERR_WORKSPACE)]:
+                     (dict(beta=ODD), A.ERR_INVALID_ARG), (dict(c=cache(rows=2000), ws=None), A.ERR_WORKSPACE),
+                     (dict(c=cache(rows=2000), ws=ODD), A.ERR_WORKSPACE),
+                     (dict(c=cache(rows=100000), n=1000), A.ERR_WORKSPACE)]:
         assert call(**kw) == want, kw
 
 
 def test_attend_qcache_workspace_size():
     size = A.attend_qcache_workspace_size
-    assert size(512, 16384, 4) > size(512, 3277, 4) > 0
-    assert size(512, 16384, 4, nsel=16) < size(512, 16384, 4)
-    assert size(1 << 20, 1 << 26, 16) > 1 << 40                        # no overflow
+    assert size(512, 16384, 4) > size(8, 16384, 4, nsel=64) > 0
+    assert size(1, 64, 4) == 0                                         # one workgroup's work
+    assert size(1 << 20, 1 << 26, 16) == 0 < size(100, 1 << 26, 16) < 1 << 26   # however large the cache
     for args, want in [((0, 1, 1), A.ERR_INVALID_ARG), ((1, 0, 1), A.ERR_INVALID_ARG), ((1, 1, 0), A.ERR_INVALID_ARG),
                        ((1, 1, 17), A.ERR_UNSUPPORTED), ((1, 1, 1, -1), A.ERR_INVALID_ARG),
                        ((1, 1, 1, 0, -1), A.ERR_INVALID_ARG), ((1, 1, 1, (1 << 20) + 1), A.ERR_UNSUPPORTED)]:

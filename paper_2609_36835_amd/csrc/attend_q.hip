@@ -120,13 +120,6 @@ __device__ inline void split_p(const float *p, Frag &h, Frag &m, Frag &l) {
   }
 }
 
-// Reductions over the four 16-lane rows (g) of a wave, every lane with the result.
-template <typename F> __device__ inline float over_rows(float x, F f) {
-  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
 // The word that lane r + FROM (mod 16) of the lane's row holds.
 template <int FROM> __device__ inline uint32_t from_lane(uint32_t x) {
   return __builtin_amdgcn_update_dpp(0u, x, 0x120 + (16 - FROM), 0xf, 0xf, true);   // rotate right by 16 - FROM
@@ -164,12 +157,6 @@ template <int N, int PARTS> __device__ inline float softmax_step(float (&sv)[N],
   return keep;
 }
 
-// Bounds-checked reads of `bytes` from p on (wave-uniform): zero behind them.
-__device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000);
-}
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 }  // namespace
 
 struct AttendQ {
@@ -235,7 +222,7 @@ __device__ inline void put_queries(const bf16x8 (&qf)[4], bf16x8 *s_q) {
 template <int W, int FMT, int GP, bool BETA, bool STREAM>
 __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end, int len, float *s_bias,
                                      const bf16x8 (&qf0)[4], bf16x8 *s_q, float &m, float &l, f32x4 (&o)[8]) {
-  constexpr int NTV = STREAM ? 2 : 0;
+  constexpr int NTV = STREAM ? kStreamed : 0;
   const int lane = threadIdx.x & 63, g = lane >> 4;
   // block and live tokens of list entry idx; none past the end
   auto block_at = [&](int idx, int &b, int &live) {
@@ -409,7 +396,7 @@ template <int NT> __device__ inline void load_tail_values(const AttendQ &a, int6
 template <int W, bool STREAM>
 __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, int len, const bf16x8 *s_q, float &m,
                                    float &l, f32x4 (&o)[8]) {
-  constexpr int NTV = STREAM ? 2 : 0;
+  constexpr int NTV = STREAM ? kStreamed : 0;
   const int lane = threadIdx.x & 63, g = lane >> 4;
   const int64_t pr = (int64_t)p * a.F;
   auto live_at = [&](int idx) { return __builtin_amdgcn_readfirstlane(idx < end ? max(0, min(len - idx * kAqTail, kAqTail)) : 0); };

@@ -15,46 +15,61 @@ namespace arckv {
 
 hipError_t launch_select(const float *scores, int B, int T, int t, int32_t *anchors, hipStream_t s);
 
+// pairs lie over a grid's y and z, whose extents are limited
+constexpr int kGridY = 32768;
+
 // ---------------------------------------------------------------- write
 // One workgroup per (block, pair, keys or values).  Thread (row group, 8 dims)
 // holds four of the block's rows in registers: the kept rows before `start`
 // from the cache, the new ones from the source, so that a block's scale is that
-// of all it holds.  One pass over memory: 2 (or 4) bytes in, 1 out per element.
+// of all it holds.  One pass over memory: 2 (or 4) bytes in, 1 out per element,
+// both as streams.  Loads go through the bounds-checked path, which gives zeros
+// for rows of the other kind, so none waits in a branch.
 template <int FMT, typename T, bool BOUNDS>
 __device__ inline void write_block(uint8_t *codes, float *scales, uint8_t *bounds, const T *src, int p, int b, int rows,
                                    int nblk, int n, int start, int end) {
   __shared__ uint32_t s_amax[4];
   __shared__ float s_bound[4][2][kHeadDim];
+  constexpr int kRow = kHeadDim * sizeof(T);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int dim = 8 * (tid & 15), row0 = b * kQBlock + (tid >> 4);   // this thread's rows: row0 + 16 i
+  const int dim = 8 * (tid & 15), r0 = tid >> 4;        // this thread's rows of the block: r0 + 16 i
+  const int row0 = b * kQBlock;
+  // the same in every lane, which a median instruction hides from the compiler
+  const int kept = __builtin_amdgcn_readfirstlane(min(max(start - row0, 0), kQBlock)),
+            held = __builtin_amdgcn_readfirstlane(min(end - row0, kQBlock));
+  uint8_t *block = codes + ((int64_t)p * rows + row0) * kHeadDim;
   float x[4][8];
-  bool held[4];
-  const float old_scale = b * kQBlock < start ? scales[(int64_t)p * nblk + b] : 0.0f;
+  {
+    const __amdgpu_buffer_rsrc_t from = buffer(src + ((int64_t)p * n + row0 + kept - start) * kHeadDim, (held - kept) * kRow);
+    u32x4 v[4][sizeof(T) / 2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 16 * i;
-    held[i] = row < end;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
-    if (row < start) {
-      const uint2 c = *reinterpret_cast<const uint2 *>(codes + ((int64_t)p * rows + row) * kHeadDim + dim);
-      float y[2][4];
-      QCode<FMT>::unpack4(c.x, y[0]);
-      QCode<FMT>::unpack4(c.y, y[1]);
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h)   // a kept row's offset is negative, so out of range
+        v[i][h] = __builtin_amdgcn_raw_buffer_load_b128(from, (r0 + 16 * i - kept) * kRow + dim * (int)sizeof(T) + 16 * h, 0, kStreamed);
+    if (kept > 0) {
+      const float old = scales[(int64_t)p * nblk + b];
+      const __amdgpu_buffer_rsrc_t before = buffer(block, kept * kHeadDim);
+      u32x2 c[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] = y[e / 4][e % 4] * old_scale;
-    } else if (row < end) {
-      const T *from = src + ((int64_t)p * n + (row - start)) * kHeadDim + dim;
-      if constexpr (sizeof(T) == 2) {
-        const bf16x8 v = *reinterpret_cast<const bf16x8 *>(from);
+      for (int i = 0; i < 4; ++i) c[i] = __builtin_amdgcn_raw_buffer_load_b64(before, (r0 + 16 * i) * kHeadDim + dim, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = (float)v[e];
-      } else {
-        const float4 a = *reinterpret_cast<const float4 *>(from), c = *reinterpret_cast<const float4 *>(from + 4);
-        x[i][0] = a.x; x[i][1] = a.y; x[i][2] = a.z; x[i][3] = a.w;
-        x[i][4] = c.x; x[i][5] = c.y; x[i][6] = c.z; x[i][7] = c.w;
+      for (int i = 0; i < 4; ++i) {
+        float y[2][4];
+        QCode<FMT>::unpack4(c[i][0], y[0]);
+        QCode<FMT>::unpack4(c[i][1], y[1]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = y[e / 4][e % 4] * old;
       }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = sizeof(T) == 2 ? __uint_as_float(e & 1 ? v[i][0][e / 2] & 0xffff0000u : v[i][0][e / 2] << 16)
+                                       : __uint_as_float(v[i][(e / 4) % (sizeof(T) / 2)][e % 4]);
+        x[i][e] = r0 + 16 * i < kept ? x[i][e] : y;
+      }
   }
   // largest magnitude as float bits: a NaN or an infinity is larger than every number
   uint32_t amax = 0;
@@ -70,16 +85,12 @@ __device__ inline void write_block(uint8_t *codes, float *scales, uint8_t *bound
     for (int e = 0; e < 8; ++e) {
       float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (held[i]) {
-          lo = fminf(lo, x[i][e]);
-          hi = fmaxf(hi, x[i][e]);
-        }
-#pragma unroll
-      for (int m = 16; m <= 32; m <<= 1) {
-        lo = fminf(lo, __shfl_xor(lo, m, 64));
-        hi = fmaxf(hi, __shfl_xor(hi, m, 64));
+      for (int i = 0; i < 4; ++i) {
+        lo = r0 + 16 * i < held ? fminf(lo, x[i][e]) : lo;
+        hi = r0 + 16 * i < held ? fmaxf(hi, x[i][e]) : hi;
       }
+      lo = over_rows(lo, [](float a, float c) { return fminf(a, c); });
+      hi = over_rows(hi, [](float a, float c) { return fmaxf(a, c); });
       if (lane < 16) {
         s_bound[wave][0][dim + e] = lo;
         s_bound[wave][1][dim + e] = hi;
@@ -94,12 +105,12 @@ __device__ inline void write_block(uint8_t *codes, float *scales, uint8_t *bound
   if (tid == 0) scales[(int64_t)p * nblk + b] = finite ? pow2f(ex) : __uint_as_float(0x7fc00000u);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (!held[i]) continue;
-    uint2 c;
-    c.x = QCode<FMT>::pack4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
-    c.y = QCode<FMT>::pack4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
-    if (!finite) c.x = c.y = 0u;
-    *reinterpret_cast<uint2 *>(codes + ((int64_t)p * rows + row0 + 16 * i) * kHeadDim + dim) = c;
+    u32x2 c;
+    c[0] = QCode<FMT>::pack4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
+    c[1] = QCode<FMT>::pack4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
+    if (!finite) c = u32x2{0u, 0u};
+    if (r0 + 16 * i < held)
+      __builtin_nontemporal_store(c, reinterpret_cast<u32x2 *>(block + (r0 + 16 * i) * kHeadDim + dim));
   }
   if constexpr (BOUNDS) {
     if (tid < 64) {
@@ -121,27 +132,25 @@ template <int FMT, typename T>
 __global__ void __launch_bounds__(256) k_qcache_write(QCache c, int n, const T *__restrict__ K, const T *__restrict__ V,
                                                       const int32_t *__restrict__ starts,
                                                       const int32_t *__restrict__ counts) {
-  for (int p = blockIdx.y; p < c.P; p += gridDim.y) {
-    const int start = starts ? min(max(starts[p], 0), c.rows) : 0;
-    const int end = min(start + clip_len(counts, p, n), c.rows);
-    const int b = start / kQBlock + blockIdx.x;
-    if (end > start && b * kQBlock < end) {
-      if (blockIdx.z)
-        write_block<FMT, T, false>(c.V, c.Vs, nullptr, V, p, b, c.rows, c.nblk, n, start, end);
-      else if (c.bounds)
-        write_block<FMT, T, true>(c.K, c.Ks, c.bounds, K, p, b, c.rows, c.nblk, n, start, end);
-      else
-        write_block<FMT, T, false>(c.K, c.Ks, nullptr, K, p, b, c.rows, c.nblk, n, start, end);
-    }
-    __syncthreads();   // the next pair's block uses the same LDS
-  }
+  const int p = (blockIdx.z >> 1) * gridDim.y + blockIdx.y;
+  if (p >= c.P) return;
+  const int start = starts ? __builtin_amdgcn_readfirstlane(min(max(starts[p], 0), c.rows)) : 0;
+  const int end = __builtin_amdgcn_readfirstlane(min(start + clip_len(counts, p, n), c.rows));
+  const int b = start / kQBlock + blockIdx.x;
+  if (end <= start || b * kQBlock >= end) return;
+  if (blockIdx.z & 1)
+    write_block<FMT, T, false>(c.V, c.Vs, nullptr, V, p, b, c.rows, c.nblk, n, start, end);
+  else if (c.bounds)
+    write_block<FMT, T, true>(c.K, c.Ks, c.bounds, K, p, b, c.rows, c.nblk, n, start, end);
+  else
+    write_block<FMT, T, false>(c.K, c.Ks, nullptr, K, p, b, c.rows, c.nblk, n, start, end);
 }
 
 hipError_t launch_qcache_write(int fmt, int dtype, const QCache &c, int n, const void *K, const void *V,
                                const int32_t *start, const int32_t *count, hipStream_t s) {
   // blocks that n rows can touch: one more than their number where they may begin inside a block
   const int spans = min(start ? (n + kQBlock - 2) / kQBlock + 1 : (n + kQBlock - 1) / kQBlock, c.nblk);
-  const dim3 grid((unsigned)spans, (unsigned)min(c.P, 65535), 2);
+  const dim3 grid((unsigned)spans, (unsigned)min(c.P, kGridY), (unsigned)(2 * ((c.P + kGridY - 1) / kGridY)));
   auto go = [&](auto kern, auto *k, auto *v) {
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, c, n, k, v, start, count);
     return hipGetLastError();
@@ -154,50 +163,57 @@ hipError_t launch_qcache_write(int fmt, int dtype, const QCache &c, int n, const
 }
 
 // ---------------------------------------------------------------- read
-// A thread turns 8 (bf16 out) or 4 (float32 out) codes of a row into 16 bytes.
+// A thread turns 8 (bf16 out) or 4 (float32 out) codes of each of four rows into
+// 16 bytes, written as a stream.
+constexpr int kReadRows = 4;
 template <int FMT, typename T>
 __global__ void __launch_bounds__(256) k_qcache_read(QCache c, int first, int n, const int32_t *__restrict__ length,
                                                      T *__restrict__ K, T *__restrict__ V) {
-  constexpr int PER = 16 / sizeof(T), LANES = kHeadDim / PER;   // codes per thread, threads per row
-  const uint8_t *codes = blockIdx.z ? c.V : c.K;
-  const float *scales = blockIdx.z ? c.Vs : c.Ks;
-  T *out = blockIdx.z ? V : K;
-  const int dim = PER * (threadIdx.x % LANES);
-  const int i = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (i >= n) return;
-  const int row = first + i;
-  for (int p = blockIdx.y; p < c.P; p += gridDim.y) {
+  constexpr int PER = 16 / sizeof(T), LANES = kHeadDim / PER, STEP = 256 / LANES;   // codes per thread; threads per row; rows at a time
+  const int p = (blockIdx.z >> 1) * gridDim.y + blockIdx.y;
+  if (p >= c.P) return;
+  const uint8_t *codes = blockIdx.z & 1 ? c.V : c.K;
+  const float *scales = (blockIdx.z & 1 ? c.Vs : c.Ks) + (int64_t)p * c.nblk;
+  T *out = (blockIdx.z & 1 ? V : K) + (int64_t)p * n * kHeadDim;
+  const int dim = PER * (threadIdx.x % LANES), i0 = blockIdx.x * (kReadRows * STEP) + threadIdx.x / LANES;
+  const int len = clip_len(length, p, c.rows);
+  uint32_t w[kReadRows][PER / 4];
+  float s[kReadRows];
+#pragma unroll
+  for (int k = 0; k < kReadRows; ++k) {
+    const int row = first + i0 + k * STEP, at = max(min(row, len - 1), 0);   // in range always; rows past the end are not used
+    s[k] = row < len ? scales[at / kQBlock] : 0.0f;
+    __builtin_memcpy(w[k], codes + ((int64_t)p * c.rows + at) * kHeadDim + dim, PER);
+  }
+#pragma unroll
+  for (int k = 0; k < kReadRows; ++k) {
+    const int i = i0 + k * STEP;
     float x[PER];
-    if (row < clip_len(length, p, c.rows)) {
-      const float s = scales[(int64_t)p * c.nblk + row / kQBlock];
-      const uint32_t *from = reinterpret_cast<const uint32_t *>(codes + ((int64_t)p * c.rows + row) * kHeadDim + dim);
 #pragma unroll
-      for (int k = 0; k < PER / 4; ++k) {
-        float y[4];
-        QCode<FMT>::unpack4(from[k], y);
+    for (int h = 0; h < PER / 4; ++h) {
+      float y[4];
+      QCode<FMT>::unpack4(w[k][h], y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * k + e] = y[e] * s;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < PER; ++e) x[e] = 0.0f;
+      for (int e = 0; e < 4; ++e) x[4 * h + e] = first + i < len ? y[e] * s[k] : 0.0f;
     }
-    T *to = out + ((int64_t)p * n + i) * kHeadDim + dim;
+    if (i >= n) continue;
+    u32x4 v;
     if constexpr (sizeof(T) == 2) {
-      bf16x8 v;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (bf16)x[e];
-      *reinterpret_cast<bf16x8 *>(to) = v;
+      for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_perm(__float_as_uint(x[2 * e + 1]), __float_as_uint(x[2 * e]), 0x07060302u);
     } else {
-      *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(x[e]);
     }
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + (int64_t)i * kHeadDim + dim));
   }
 }
 
 hipError_t launch_qcache_read(int fmt, int dtype, const QCache &c, int first, int n, const int32_t *length, void *K,
                               void *V, hipStream_t s) {
-  const int per_wg = 256 / (kHeadDim / (dtype == ARCKV_BF16 ? 8 : 4));
-  const dim3 grid((unsigned)((n + per_wg - 1) / per_wg), (unsigned)min(c.P, 65535), 2);
+  const int per_wg = kReadRows * 256 / (kHeadDim / (dtype == ARCKV_BF16 ? 8 : 4));
+  const dim3 grid((unsigned)((n + per_wg - 1) / per_wg), (unsigned)min(c.P, kGridY),
+                  (unsigned)(2 * ((c.P + kGridY - 1) / kGridY)));
   auto go = [&](auto kern, auto *k, auto *v) {
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, c, first, n, length, k, v);
     return hipGetLastError();
@@ -396,7 +412,7 @@ __global__ void __launch_bounds__(256) k_block_scores(QCache c, int G, double sc
 
 hipError_t launch_select_blocks(int fmt, const QCache &c, int G, double scale, const void *Q, const float *beta,
                                 const int32_t *length, int k, float *scores, int32_t *blocks, hipStream_t s) {
-  const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
+  const unsigned py = (unsigned)min(c.P, kGridY), pz = (unsigned)((c.P + kGridY - 1) / kGridY);
   const dim3 grid((unsigned)((c.nblk + 4 * kBsTile - 1) / (4 * kBsTile)), py, pz);
   auto go = [&](auto kern) {
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, c, G, scale, (const bf16 *)Q, beta, length, scores);

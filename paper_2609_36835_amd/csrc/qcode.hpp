@@ -46,6 +46,22 @@ template <> struct QCode<ARCKV_INT8> {
   }
 };
 
+// Bounds-checked reads of `bytes` from p on (wave-uniform): zero behind them.
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000);
+}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+constexpr int kStreamed = 2;   // a load's or store's aux bits: not kept in the caches
+
+// Reduction over the four 16-lane rows of a wave, every lane with the result.
+template <typename F> __device__ inline float over_rows(float x, F f) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
 // 2^e for e in [-126, 127]
 __device__ inline float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 

@@ -251,9 +251,6 @@ template <int CTRL> __device__ inline double dpp(double x) {
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 constexpr int kDppXor1 = 0xb1, kDppXor2 = 0x4e, kDppRor4 = 0x124, kDppRor8 = 0x128;
-// the larger; a NaN wins
-__device__ inline double nan_max(double a, double b) { return a > b || a != a ? a : b; }
-
 __device__ inline f32x4 mfma_f16(f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
@@ -286,147 +283,243 @@ template <int FMT> __device__ inline void code_parts(uint32_t w0, uint32_t w1, f
   if constexpr (FMT == ARCKV_E4M3) __builtin_memcpy(&rest, low, 16);
 }
 
-// CT: tiles of 16 columns, four query rows each.  A wave takes tiles of 16 blocks; blockIdx.x strides over them.
+// A pair's query planes in LDS and their exponents.  CT: tiles of 16 columns, four query rows each.
+constexpr int kNoQuery = INT32_MIN, kBadQuery = INT32_MAX;   // in the place of an exponent: no row; a non-finite one
+template <int CT> struct Planes {
+  f16 d[2][16 * CT][kHeadDim + 8];   // of q+ and q-, row = column 4 g + t; padded for the banks
+  int e[4 * CT];
+};
+
+// A wave a query row, two channels a lane; the workgroup meets afterwards.
+template <int CT> __device__ inline void make_planes(const bf16 *Q, int G, Planes<CT> &pl) {
+  const int lane = threadIdx.x & 63;
+  uint32_t word[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int g = 4 * ct + (threadIdx.x >> 6);
+    word[ct] = g < G ? reinterpret_cast<const uint32_t *>(Q + g * kHeadDim)[lane] : 0u;
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int g = 4 * ct + (threadIdx.x >> 6);
+    const float q[2] = {__uint_as_float(word[ct] << 16), __uint_as_float(word[ct] & 0xffff0000u)};
+    uint32_t amax = max(__float_as_uint(q[0]) & 0x7fffffffu, __float_as_uint(q[1]) & 0x7fffffffu);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
+    const bool finite = amax < 0x7f800000u;
+    int E = 0;
+    if (finite && amax) E = __builtin_amdgcn_frexp_expf(__uint_as_float(amax));   // amax < 2^E
+    if (lane == 0) pl.e[g] = g >= G ? kNoQuery : finite ? E : kBadQuery;
+    float x[2] = {ldexpf(q[0], 8 - E), ldexpf(q[1], 8 - E)};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f16x2 plus, minus;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float n = finite ? truncf(x[e]) : 0.0f;
+        plus[e] = (f16)fmaxf(n, 0.0f);
+        minus[e] = (f16)fminf(n, 0.0f);
+        x[e] = (x[e] - n) * 256.0f;
+      }
+      *reinterpret_cast<f16x2 *>(&pl.d[0][4 * g + t][2 * lane]) = plus;
+      *reinterpret_cast<f16x2 *>(&pl.d[1][4 * g + t][2 * lane]) = minus;
+    }
+  }
+  __syncthreads();
+}
+
+// The tile's bounds that a lane needs: block r's, bytes 64 kk + 16 kg .. + 15.
+struct TileBounds {
+  uint4 lo[2], hi[2];
+};
+__device__ inline TileBounds load_bounds(const QCache &c, int p, int tile) {
+  const int lane = threadIdx.x & 63, b = min(tile * kBsTile + (lane & 15), c.nblk - 1);
+  const uint8_t *row = c.bounds + ((int64_t)p * c.nblk + b) * 2 * kHeadDim + 16 * (lane >> 4);
+  TileBounds t;
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    t.lo[kk] = *reinterpret_cast<const uint4 *>(row + 64 * kk);
+    t.hi[kk] = *reinterpret_cast<const uint4 *>(row + kHeadDim + 64 * kk);
+  }
+  return t;
+}
+
+// A wave's scores of the tile's 16 blocks: lane 16 kg + j (j < 4) returns block 4 kg + j's.
+template <int FMT, int CT, bool BETA>
+__device__ inline float tile_scores(const QCache &c, const TileBounds &t, int p, int tile, int len, int G, double scale,
+                                    const float *beta, const Planes<CT> &pl) {
+  const int lane = threadIdx.x & 63, kg = lane >> 4, r = lane & 15, b0 = tile * kBsTile;
+  if (b0 * kQBlock >= len) return -INFINITY;
+  const int b = b0 + 4 * kg + (r & 3);   // this lane's output
+  const bool there = b < c.nblk && b * kQBlock < len;
+  const double kscale = there ? scale * (double)c.Ks[(int64_t)p * c.nblk + b] : 0.0;
+  float top = -INFINITY;
+  if constexpr (BETA) {
+    // four lanes a block, 16 biases each; a NaN wins
+    const int j0 = (b0 + (lane >> 2)) * kQBlock + 16 * (lane & 3), j1 = min(j0 + 16, len);
+    for (int j = j0; j < j1; ++j) {
+      const float x = beta[(int64_t)p * c.rows + j];
+      top = x > top || x != x ? x : top;
+    }
+#pragma unroll
+    for (int m = 1; m <= 2; m <<= 1) {
+      const float x = __shfl_xor(top, m, 64);
+      top = x > top || x != x ? x : top;
+    }
+    top = __shfl(top, 4 * (4 * kg + (r & 3)), 64);
+  }
+  f32x4 acc[CT][2] = {};
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    // channels 64 kk + 16 kg + 8 h .. + 7, as the codes were read
+    const int kk = ks / 2, h = ks % 2, d = 64 * kk + 16 * kg + 8 * h;
+    f16x8 hn, hr, ln, lr;
+    code_parts<FMT>(h ? t.hi[kk].z : t.hi[kk].x, h ? t.hi[kk].w : t.hi[kk].y, hn, hr);
+    code_parts<FMT>(h ? t.lo[kk].z : t.lo[kk].x, h ? t.lo[kk].w : t.lo[kk].y, ln, lr);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      const f16x8 qp = *reinterpret_cast<const f16x8 *>(&pl.d[0][16 * ct + r][d]),
+                  qn = *reinterpret_cast<const f16x8 *>(&pl.d[1][16 * ct + r][d]);
+      acc[ct][0] = mfma_f16(ln, qn, mfma_f16(hn, qp, acc[ct][0]));
+      if constexpr (FMT == ARCKV_E4M3) acc[ct][1] = mfma_f16(lr, qn, mfma_f16(hr, qp, acc[ct][1]));
+    }
+  }
+  double best = 0.0, weight[CT];
+  bool bad = false;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int e = pl.e[4 * ct + (r >> 2)];
+    weight[ct] = e == kNoQuery ? 0.0 : ldexp(1.0, e - 8 * ((r & 3) + 1));
+    bad |= e == kBadQuery;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {   // blocks 4 kg + j
+    double m = -INFINITY;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      double x = (double)acc[ct][0][j];
+      if constexpr (FMT == ARCKV_E4M3) x += (double)acc[ct][1][j];
+      x *= weight[ct];
+      x += dpp<kDppXor1>(x);
+      x += dpp<kDppXor2>(x);
+      m = fmax(m, weight[ct] > 0.0 ? x : -INFINITY);   // a row that is not there never is the largest
+    }
+    m = fmax(m, dpp<kDppRor4>(m));
+    m = fmax(m, dpp<kDppRor8>(m));
+    best = (r & 3) == j ? m : best;
+  }
+  if (__any(bad)) best = __longlong_as_double(0x7ff8000000000000ll);   // a non-finite query gives NaN scores
+  double score = best * kscale;
+  if constexpr (BETA) score = top == -INFINITY ? -INFINITY : score + (double)top;
+  return there ? (float)score : -INFINITY;
+}
+
+// A wave per tile of 16 blocks and step, whose bounds are on their way while the workgroup makes its planes or the wave
+// is at the tile before.
 template <int FMT, int CT, bool BETA>
 __global__ void __launch_bounds__(256) k_block_scores(QCache c, int G, double scale, const bf16 *__restrict__ Q,
                                                       const float *__restrict__ beta,
                                                       const int32_t *__restrict__ length,
                                                       float *__restrict__ scores) {
-  __shared__ __align__(16) f16 sD[2][16 * CT][kHeadDim + 8];   // planes of q+ and q-, row = column 4 g + t; padded for the banks
-  __shared__ int sE[4 * CT];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kg = lane >> 4, r = lane & 15;
-  const int p = blockIdx.z * gridDim.y + blockIdx.y;
+  __shared__ __align__(16) Planes<CT> pl;
+  const int p = blockIdx.z * gridDim.y + blockIdx.y, lane = threadIdx.x & 63;
   if (p >= c.P) return;
+  int tile = blockIdx.x * 4 + (threadIdx.x >> 6);
+  TileBounds t = load_bounds(c, p, tile);
   const int len = clip_len(length, p, c.rows);
-  // ---- the planes: 16 threads a query row, 8 channels each
-  if (tid < 64 * CT) {
-    const int g = tid >> 4, d = 8 * (tid & 15);
-    bf16x8 q = {};
-    if (g < G) q = *reinterpret_cast<const bf16x8 *>(Q + ((int64_t)p * G + g) * kHeadDim + d);
-    uint32_t amax = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint((float)q[e]) & 0x7fffffffu);
-#pragma unroll
-    for (int m = 1; m < 16; m <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
-    const bool finite = amax < 0x7f800000u;
-    int E = 0;
-    if (finite && amax) E = __builtin_amdgcn_frexp_expf(__uint_as_float(amax));   // amax < 2^E
-    if ((tid & 15) == 0) sE[g] = E;
-    f16x8 plane[4][2];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float x = ldexpf((float)q[e], 8 - E);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float n = finite ? truncf(x) : __uint_as_float(0x7fc00000u);   // a non-finite query gives NaN scores
-        plane[t][0][e] = (f16)(n > 0.0f || n != n ? n : 0.0f);
-        plane[t][1][e] = (f16)(n < 0.0f ? n : 0.0f);
-        x = (x - n) * 256.0f;
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) *reinterpret_cast<f16x8 *>(&sD[s][4 * g + t][d]) = plane[t][s];
+  make_planes<CT>(Q + (int64_t)p * G * kHeadDim, G, pl);
+  while (tile * kBsTile < c.nblk) {
+    const int next = tile + 4 * gridDim.x;
+    const TileBounds ahead = load_bounds(c, p, next);
+    const float score = tile_scores<FMT, CT, BETA>(c, t, p, tile, len, G, scale, beta, pl);
+    const int b = tile * kBsTile + 4 * (lane >> 4) + (lane & 15);
+    if ((lane & 15) < 4 && b < c.nblk) scores[(int64_t)p * c.nblk + b] = score;
+    t = ahead;
+    tile = next;
   }
-  __syncthreads();
-  // weights of this lane's columns; a row that is not there never is the largest
-  double weight[CT], floor_[CT];
+}
+
+// The k largest of up to 64 KEYS scores of a pair, by one wave, in launch_select's order: larger first, ties to the lower
+// index, NaN below every number.  The k-th largest key is found two bits at a time from the top, by counting (ballots)
+// the keys at or above the three candidates; then every lane writes the indices of its keys above it, and of those equal
+// to it as many as are still wanted.  Lane l has the keys l per .. l per + per - 1, so the output ascends.
+template <int KEYS>
+__global__ void __launch_bounds__(256) k_pick_blocks(const float *__restrict__ scores, int P, int n, int k,
+                                                     int32_t *__restrict__ blocks) {
+  const int p = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (p >= P) return;
+  const int per = (n + 63) / 64;
+  uint32_t key[KEYS];
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int g = 4 * ct + (r >> 2);
-    weight[ct] = ldexp(1.0, sE[g] - 8 * ((r & 3) + 1));
-    floor_[ct] = g < G ? 0.0 : -INFINITY;
+  for (int i = 0; i < KEYS; ++i) {
+    const int at = lane * per + i;
+    key[i] = i < per && at < n ? score_key(scores[(int64_t)p * n + at]) : 0u;   // 0 is a NaN's key: see below
   }
-  const int tiles = (c.nblk + kBsTile - 1) / kBsTile;
-  for (int tile = blockIdx.x * 4 + wave; tile < tiles; tile += gridDim.x * 4) {
-    const int b0 = tile * kBsTile;
-    if (b0 * kQBlock >= len) {
-      if (lane < kBsTile && b0 + lane < c.nblk) scores[(int64_t)p * c.nblk + b0 + lane] = -INFINITY;
-      continue;
-    }
-    const uint8_t *row = c.bounds + ((int64_t)p * c.nblk + min(b0 + r, c.nblk - 1)) * 2 * kHeadDim + 16 * kg;
-    uint4 lo[2], hi[2];
+  // Keys that are not there count like NaNs, but only at candidate 0, which is not counted.
+  uint32_t kth = 0;
+  for (int shift = 30; shift >= 0; shift -= 2) {
+    int count[3] = {0, 0, 0};
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      lo[kk] = *reinterpret_cast<const uint4 *>(row + 64 * kk);
-      hi[kk] = *reinterpret_cast<const uint4 *>(row + kHeadDim + 64 * kk);
-    }
-    // this lane's output: block 4 kg + r of the tile (r < 4)
-    const int b = b0 + 4 * kg + (r & 3);
-    const bool there = b < c.nblk && b * kQBlock < len;
-    const double kscale = there ? scale * (double)c.Ks[(int64_t)p * c.nblk + b] : 0.0;
-    float top = -INFINITY;
-    if constexpr (BETA) {
-      // four lanes a block, 16 biases each
-      const int bb = b0 + (lane >> 2), j0 = bb * kQBlock + 16 * (lane & 3), j1 = min(j0 + 16, len);
-      for (int j = j0; j < j1; ++j) {
-        const float x = beta[(int64_t)p * c.rows + j];
-        top = x > top || x != x ? x : top;
-      }
+    for (int i = 0; i < KEYS; ++i)
 #pragma unroll
-      for (int m = 1; m <= 2; m <<= 1) {
-        const float x = __shfl_xor(top, m, 64);
-        top = x > top || x != x ? x : top;
-      }
-      top = __shfl(top, 4 * (4 * kg + (r & 3)), 64);
-    }
-    f32x4 acc[CT][2] = {};
+      for (int d = 0; d < 3; ++d) count[d] += __popcll(__ballot(key[i] >= (kth | (uint32_t)(d + 1) << shift)));
+    kth |= (uint32_t)(count[2] >= k ? 3 : count[1] >= k ? 2 : count[0] >= k ? 1 : 0) << shift;
+  }
+  uint32_t above = 0, equal = 0;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      // channels 64 kk + 16 kg + 8 h .. + 7, as the codes were read
-      const int kk = ks / 2, h = ks % 2, d = 64 * kk + 16 * kg + 8 * h;
-      f16x8 hn, hr, ln, lr;
-      code_parts<FMT>(h ? hi[kk].z : hi[kk].x, h ? hi[kk].w : hi[kk].y, hn, hr);
-      code_parts<FMT>(h ? lo[kk].z : lo[kk].x, h ? lo[kk].w : lo[kk].y, ln, lr);
+  for (int i = 0; i < KEYS; ++i) {
+    const bool in = i < per && lane * per + i < n;
+    above += in && key[i] > kth;
+    equal += in && key[i] == kth;
+  }
+  const uint32_t both = above << 16 | equal;   // at most 64 KEYS each
+  uint32_t sum = both;
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        const f16x8 qp = *reinterpret_cast<const f16x8 *>(&sD[0][16 * ct + r][d]),
-                    qn = *reinterpret_cast<const f16x8 *>(&sD[1][16 * ct + r][d]);
-        acc[ct][0] = mfma_f16(ln, qn, mfma_f16(hn, qp, acc[ct][0]));
-        if constexpr (FMT == ARCKV_E4M3) acc[ct][1] = mfma_f16(lr, qn, mfma_f16(hr, qp, acc[ct][1]));
-      }
-    }
-    double best = 0.0;
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t x = __shfl_up(sum, off, 64);
+    sum += lane >= off ? x : 0u;
+  }
+  const uint32_t before = sum - both, wanted = (uint32_t)k - (__shfl(sum, 63, 64) >> 16);   // of the equal ones
+  uint32_t seen = before & 0xffffu, at = (before >> 16) + min(seen, wanted);
+  int32_t *out = blocks + (int64_t)p * k;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {   // blocks 4 kg + j
-      double m = -INFINITY;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        double x = (double)acc[ct][0][j];
-        if constexpr (FMT == ARCKV_E4M3) x += (double)acc[ct][1][j];
-        x *= weight[ct];
-        x += dpp<kDppXor1>(x);
-        x += dpp<kDppXor2>(x);
-        m = nan_max(m, x + floor_[ct]);
-      }
-      m = nan_max(m, dpp<kDppRor4>(m));
-      m = nan_max(m, dpp<kDppRor8>(m));
-      best = (r & 3) == j ? m : best;
-    }
-    double score = best * kscale;
-    if constexpr (BETA) score = top == -INFINITY ? -INFINITY : score + (double)top;
-    if (r < 4 && b < c.nblk) scores[(int64_t)p * c.nblk + b] = there ? (float)score : -INFINITY;
+  for (int i = 0; i < KEYS; ++i) {
+    const bool in = i < per && lane * per + i < n, eq = in && key[i] == kth;
+    if (in && (key[i] > kth || (eq && seen < wanted))) out[at++] = lane * per + i;
+    seen += eq;
   }
 }
 
 hipError_t launch_select_blocks(int fmt, const QCache &c, int G, double scale, const void *Q, const float *beta,
                                 const int32_t *length, int k, float *scores, int32_t *blocks, hipStream_t s) {
   const unsigned py = (unsigned)min(c.P, kGridY), pz = (unsigned)((c.P + kGridY - 1) / kGridY);
-  const dim3 grid((unsigned)((c.nblk + 4 * kBsTile - 1) / (4 * kBsTile)), py, pz);
-  auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, c, G, scale, (const bf16 *)Q, beta, length, scores);
+  // two tiles a wave where that leaves the CUs four workgroups each: the planes are made once for both
+  const int by4 = (c.nblk + 4 * kBsTile - 1) / (4 * kBsTile);
+  const dim3 grid((unsigned)((int64_t)c.P * by4 > 2048 - 1 ? (by4 + 2 - 1) / 2 : by4), py, pz);
+  auto by_tiles = [&](auto fm, auto ct, auto bt) {
+    constexpr int FMT = decltype(fm)::value, CT = decltype(ct)::value;
+    constexpr bool BETA = decltype(bt)::value;
+    hipLaunchKernelGGL((k_block_scores<FMT, CT, BETA>), grid, dim3(256), 0, s, c, G, scale, (const bf16 *)Q, beta, length,
+                       scores);
     return hipGetLastError();
   };
   auto by_rows = [&](auto fm, auto bt) {
-    constexpr int FMT = decltype(fm)::value;
-    constexpr bool BETA = decltype(bt)::value;
-    return G <= 4 ? go(k_block_scores<FMT, 1, BETA>) : G <= 8 ? go(k_block_scores<FMT, 2, BETA>) : go(k_block_scores<FMT, 4, BETA>);
+    return G <= 4 ? by_tiles(fm, std::integral_constant<int, 1>{}, bt)
+                  : G <= 8 ? by_tiles(fm, std::integral_constant<int, 2>{}, bt) : by_tiles(fm, std::integral_constant<int, 4>{}, bt);
   };
   auto by_beta = [&](auto fm) { return beta ? by_rows(fm, std::true_type{}) : by_rows(fm, std::false_type{}); };
   const hipError_t e = fmt == ARCKV_E4M3 ? by_beta(std::integral_constant<int, ARCKV_E4M3>{})
                                          : by_beta(std::integral_constant<int, ARCKV_INT8>{});
-  return e != hipSuccess ? e : launch_select(scores, c.P, c.nblk, k, blocks, s);
+  if (e != hipSuccess) return e;
+  // a wave per pair up to 512 blocks (256 blocks of 512 pairs 4.3 us, 512 of 256 pairs 7.2 us; 10.7 and 8.0 us in a
+  // workgroup of 16 waves), where its counts are the longer part beyond (1024 of 8 pairs 16 us, 8 us)
+  auto pick = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)((c.P + 3) / 4)), dim3(256), 0, s, scores, c.P, c.nblk, k, blocks);
+    return hipGetLastError();
+  };
+  if (c.nblk <= 256) return pick(k_pick_blocks<4>);
+  if (c.nblk <= 512) return pick(k_pick_blocks<8>);
+  return launch_select(scores, c.P, c.nblk, k, blocks, s);
 }
 
 }  // namespace arckv

@@ -20,10 +20,10 @@
 //                      in flight each.  The waves' (max, sum, o) are merged in LDS.
 //   k_attendq_combine  merges the partials of a pair; a call of one chunk per
 //                      pair needs none.
-// 512 pairs of 3277 rows with bias and 256 tail rows take 80 us (6.1 TB/s; 93 us with
-// one block per wave and the tail in workgroups of its own, 145 us with loads
-// under branches), of 8192 to 16384 rows 272 us (6.0 TB/s; 314, 495).  Reading alone
-// reaches 6.9 TB/s.
+// 512 pairs of 3277 int8 rows with bias and 256 tail rows take 74 us (6.6 TB/s; 77 us
+// with half lines of keys per load, 93 us with one block per wave and the tail in
+// workgroups of its own, 145 us with loads under branches), of 8192 to 16384 e4m3 rows
+// 261 us (6.2 TB/s; 272, 314, 495).  Reading alone reaches 6.9 TB/s.
 #include <type_traits>
 
 #include "qcode.hpp"
@@ -36,7 +36,9 @@ constexpr int kAqWide = 16;           // of one that takes a whole pair of a sma
 constexpr int kAqSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
 constexpr int kAqStart = 6;           // cost of a workgroup beside its blocks, in blocks per wave
 constexpr int kAqTail = 32;           // tail rows per wave
-// Bytes of codes above which the values are read as a stream that the caches do not keep: the last-level cache's size.
+// Bytes of codes above which keys and values are read as streams that the caches do not keep: a quarter of the last-level
+// cache, which a decode step's other layers pass through before a layer's turn comes again.  Three caches in turn, kept and
+// streamed (values alone): 64 pairs of 4096 rows (67 MB) 16.1 and 16.5 us, of 6000 23.5 and 22.7, of 8192 31.8 and 27.8.
 constexpr int64_t kAttendKept = (int64_t)64 << 20;
 
 __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -59,33 +61,40 @@ __device__ inline uint32_t lower_halves(uint32_t first, uint32_t second) {
   return __builtin_amdgcn_perm(second, first, 0x05040100u);
 }
 
-// Codes as MFMA operands, two to a word: keys as bf16 (the queries' type), values as fp16.  Every code is exact in both.
+// Codes as MFMA operands, two to a word: four of a key as bf16 (the queries' type); those of four dims of two tokens
+// side by side, dim by dim, as fp16.  Every code is exact in both.
 template <int FMT> struct Operand;
 
 template <> struct Operand<ARCKV_E4M3> {
-  __device__ static inline void bf16x4(uint32_t w, uint32_t &first, uint32_t &second) {
+  __device__ static inline void keys(uint32_t w, uint32_t &first, uint32_t &second) {
     first = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
     second = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
   }
-  __device__ static inline void f16x4(uint32_t w, uint32_t &first, uint32_t &second) {
-    first = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
-    second = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+  __device__ static inline void values(uint32_t x, uint32_t y, uint32_t (&dim)[4]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t w = __builtin_amdgcn_perm(y, x, h ? 0x07030602u : 0x05010400u);   // x, y, x, y
+      dim[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+      dim[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+    }
   }
 };
 
 template <> struct Operand<ARCKV_INT8> {
-  __device__ static inline void bf16x4(uint32_t w, uint32_t &first, uint32_t &second) {
+  __device__ static inline void keys(uint32_t w, uint32_t &first, uint32_t &second) {
     float y[4];
     QCode<ARCKV_INT8>::unpack4(w, y);
     first = upper_halves(__float_as_uint(y[0]), __float_as_uint(y[1]));
     second = upper_halves(__float_as_uint(y[2]), __float_as_uint(y[3]));
   }
   // a byte u below fp16's exponent of 1024 is 1024 + u; with the code's sign bit flipped u is code + 128
-  __device__ static inline void f16x4(uint32_t w, uint32_t &first, uint32_t &second) {
+  __device__ static inline void values(uint32_t x, uint32_t y, uint32_t (&dim)[4]) {
     const f16x2 off = {(f16)-1152.0f, (f16)-1152.0f};
-    w ^= 0x80808080u;
-    first = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) + off);
-    second = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) + off);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t w = __builtin_amdgcn_perm(y, x, 0x0c040c00u + 0x10001u * e) ^ 0x64806480u;   // 0x0c: a zero byte
+      dim[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w) + off);
+    }
   }
 };
 
@@ -174,11 +183,13 @@ struct AttendQ {
   int iters, nch;             // units (blocks, 32 tail rows) per wave of a chunk; chunks per pair
 };
 
-// What a wave has in flight of a block of 64 tokens.  Keys as MFMA rows, where a contraction step pairs bytes
-// 64 kk + 16 g + 8 h .. + 7 of keys and queries, so that a lane reads 16 bytes at a time; values for the lane of keys
-// 16 (i / 4) + 4 g + i % 4 (those of its logits) and dims 8 r .. 8 r + 7.
+// What a wave has in flight of a block of 64 tokens.  Keys feed MFMA as rows, where a contraction step pairs bytes
+// 64 kk + 16 g + 8 h .. + 7 of keys and queries; values are the lane's of keys 16 (i / 4) + 4 g + i % 4 (those of its
+// logits) and dims 8 r .. 8 r + 7.  MFMA gives a key row to four lanes, so its 128 bytes would take two loads of half a
+// line each; as a stream a line is then fetched twice.  LINES: a load takes 8 whole rows, 16 bytes a lane in order, and
+// the rows find their lanes through LDS that only this wave uses: 512 pairs of 8192 to 16384 rows 261 us instead of 272.
 struct Keys {
-  u32x4 c[4][2];
+  u32x4 c[4][2];   // LINES: c[i / 2][i % 2] is row 8 i + lane / 8, piece lane % 8
   float scale, bias;
 };
 struct Values {
@@ -187,18 +198,35 @@ struct Values {
 };
 
 // Loads of block b of pair p, `live` of its tokens in use (both the wave's); none where live is 0, and zeros behind them.
-template <bool BETA>
+template <bool BETA, bool LINES, int NT>
 __device__ inline void load_keys(const AttendQ &a, int64_t pair_block, int64_t row0, int live, Keys &k) {
-  const int lane = threadIdx.x & 63, at = (lane & 15) * kHeadDim + 16 * (lane >> 4);
+  const int lane = threadIdx.x & 63, at = LINES ? 16 * lane : (lane & 15) * kHeadDim + 16 * (lane >> 4);
   const __amdgpu_buffer_rsrc_t kb = buffer(a.c.K + row0 * kHeadDim, live * kHeadDim);
 #pragma unroll
   for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
-      k.c[kt][kk] = __builtin_amdgcn_raw_buffer_load_b128(kb, at + 16 * kHeadDim * (kt % 2) + 64 * kk, 4096 * (kt / 2), 0);
+      k.c[kt][kk] = __builtin_amdgcn_raw_buffer_load_b128(kb, at + 16 * kHeadDim * (kt % 2) + (LINES ? 8 * kHeadDim : 64) * kk,
+                                                          4096 * (kt / 2), LINES ? NT : 0);
   k.scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer(a.c.Ks + pair_block, live ? 4 : 0), 0, 0, 0));
   if constexpr (BETA)
     k.bias = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer(a.beta + row0, live * 4), 4 * lane, 0, 0));
+}
+
+// Rows in order to LDS; the 16-byte pieces of row n lie at piece ^ (n / 2 % 8), so that the lanes of a key column, 16 rows
+// apart in nothing but the row, meet different banks.
+__device__ inline void put_keys(const Keys &k, u32x4 *s_k) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = 8 * i + (lane >> 3);
+    s_k[row * 8 + ((lane & 7) ^ (row >> 1 & 7))] = k.c[i / 2][i % 2];
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+__device__ inline u32x4 get_keys(const u32x4 *s_k, int kt, int kk) {
+  const int lane = threadIdx.x & 63, row = 16 * kt + (lane & 15);
+  return s_k[row * 8 + ((4 * kk + (lane >> 4)) ^ (row >> 1 & 7))];
 }
 
 template <int NT>
@@ -221,8 +249,10 @@ __device__ inline void put_queries(const bf16x8 (&qf)[4], bf16x8 *s_q) {
 // The blocks first, first + W, ... below end of the list (or of the cache), a wave's share of a chunk.
 template <int W, int FMT, int GP, bool BETA, bool STREAM>
 __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end, int len, float *s_bias,
-                                     const bf16x8 (&qf0)[4], bf16x8 *s_q, float &m, float &l, f32x4 (&o)[8]) {
+                                     const bf16x8 (&qf0)[4], bf16x8 *s_q, u32x4 *s_k, float &m, float &l,
+                                     f32x4 (&o)[8]) {
   constexpr int NTV = STREAM ? kStreamed : 0;
+  constexpr bool LINES = W != kAqWide;   // 16 waves have no room in LDS
   const int lane = threadIdx.x & 63, g = lane >> 4;
   // block and live tokens of list entry idx; none past the end
   auto block_at = [&](int idx, int &b, int &live) {
@@ -237,7 +267,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
   Keys k;
   Values v;
   const int64_t pb = (int64_t)p * a.c.nblk, pr = (int64_t)p * a.c.rows;
-  load_keys<BETA>(a, pb + b, pr + (int64_t)b * kQBlock, live, k);
+  load_keys<BETA, LINES, NTV>(a, pb + b, pr + (int64_t)b * kQBlock, live, k);
   load_values<NTV>(a, pb + b, pr + (int64_t)b * kQBlock, live, v);
   __builtin_amdgcn_sched_barrier(0);
   put_queries(qf0, s_q);
@@ -251,16 +281,17 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
     bf16x8 qf[4];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) qf[ks] = s_q[ks * 64 + lane];
+    if constexpr (LINES) put_keys(k, s_k);
     f32x4 dots[4];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
-        const u32x4 c = k.c[kt][ks / 2];
+        const u32x4 c = LINES ? get_keys(s_k, kt, ks / 2) : k.c[kt][ks / 2];
         Frag f;
-        Operand<FMT>::bf16x4(c[2 * (ks % 2)], f.w[0], f.w[1]);
-        Operand<FMT>::bf16x4(c[2 * (ks % 2) + 1], f.w[2], f.w[3]);
+        Operand<FMT>::keys(c[2 * (ks % 2)], f.w[0], f.w[1]);
+        Operand<FMT>::keys(c[2 * (ks % 2) + 1], f.w[2], f.w[3]);
         acc = mfma16(f.v, qf[ks], acc);
       }
       dots[kt] = acc;
@@ -295,7 +326,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
     }
     if constexpr (BETA) __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (W != kAqWide) load_keys<BETA>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
+    if constexpr (W != kAqWide) load_keys<BETA, LINES, NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
     __builtin_amdgcn_sched_barrier(0);
     bool any;
     const float keep = softmax_step<N, PARTS>(sv, m, l, any);
@@ -351,9 +382,10 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
 #pragma unroll
         for (int kq = 0; kq < 4; ++kq) {
           const uint32_t x = v.c[8 * half + 2 * kq][dd], y = v.c[8 * half + 2 * kq + 1][dd];
-          // bytes of two keys side by side: dims 4 dd, 4 dd + 1, then 4 dd + 2, 4 dd + 3
-          Operand<FMT>::f16x4(__builtin_amdgcn_perm(y, x, 0x05010400u), vf[0].w[kq], vf[1].w[kq]);
-          Operand<FMT>::f16x4(__builtin_amdgcn_perm(y, x, 0x07030602u), vf[2].w[kq], vf[3].w[kq]);
+          uint32_t w[4];
+          Operand<FMT>::values(x, y, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vf[e].w[kq] = w[e];
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = mfma16h(vf[e].v, ph[half].v, mfma16h(vf[e].v, pl[half].v, acc[e]));
@@ -446,9 +478,12 @@ __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, 
 // GP: the query rows that LDS and operands have room for, G <= GP <= 16.
 template <int W, int FMT, int GP, bool BETA, bool STREAM>
 __global__ void __launch_bounds__(64 * W, W == kAqW ? 3 : 4) k_attendq_partial(AttendQ a) {
-  // a wave's query operands, [step][lane], and in their place its sums once they are complete
+  // a wave's query operands, [step][lane], and a block's keys; in their place its sums once they are complete
   union Own {
-    bf16x8 q[4 * 64];
+    struct {
+      bf16x8 q[4 * 64];
+      u32x4 k[W == kAqWide ? 1 : kQBlock * kHeadDim / 16];
+    };
     float o[GP][kHeadDim];
   };
   __shared__ __align__(16) Own sOwn[W];
@@ -469,7 +504,7 @@ __global__ void __launch_bounds__(64 * W, W == kAqW ? 3 : 4) k_attendq_partial(A
   const int len = clip_len(a.length, p, a.c.rows);
   const int bend = min(end, a.blocks ? a.nsel : (len + kQBlock - 1) / kQBlock);
   if (first < bend)
-    attend_blocks<W, FMT, GP, BETA, STREAM>(a, p, first, bend, len, sB[BETA ? wave : 0], qf, sOwn[wave].q, m, l, o);
+    attend_blocks<W, FMT, GP, BETA, STREAM>(a, p, first, bend, len, sB[BETA ? wave : 0], qf, sOwn[wave].q, sOwn[wave].k, m, l, o);
   else
     put_queries(qf, sOwn[wave].q);
   if (end > a.nsel) {
@@ -579,8 +614,8 @@ static bool attendq_small(int P, int nsel, int F) {
 
 // Chunks per pair, and the units (blocks and 32-row pieces of the tail) per wave of one.  Workgroups run kAqSlots at a
 // time, so a call takes as many rounds as they fill, of a workgroup's units and its start each; the number of chunks with
-// the least sum is taken: 512 pairs of 3277 + 256 rows 80 us as one chunk each (96 us as three), of 8192 to 16384 rows
-// 272 us as three.
+// the least sum is taken: 512 pairs of 3277 + 256 rows in one chunk each took 80 us where three took 96; 8192 to 16384
+// rows go in three.
 int attendq_chunks(int P, int nsel, int F, int *iters) {
   const int units = nsel + (F + kAqTail - 1) / kAqTail;
   if (attendq_small(P, nsel, F)) {

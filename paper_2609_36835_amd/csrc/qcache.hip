@@ -439,53 +439,73 @@ __global__ void __launch_bounds__(256) k_block_scores(QCache c, int G, double sc
   }
 }
 
-// The k largest of up to 64 KEYS scores of a pair, by one wave, in launch_select's order: larger first, ties to the lower
-// index, NaN below every number.  The k-th largest key is found two bits at a time from the top, by counting (ballots)
-// the keys at or above the three candidates; then every lane writes the indices of its keys above it, and of those equal
-// to it as many as are still wanted.  Lane l has the keys l per .. l per + per - 1, so the output ascends.
-template <int KEYS>
-__global__ void __launch_bounds__(256) k_pick_blocks(const float *__restrict__ scores, int P, int n, int k,
-                                                     int32_t *__restrict__ blocks) {
-  const int p = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+// The k largest of a pair's n scores in launch_select's order: larger first, ties to the lower index, NaN below every
+// number.  WAVES of a workgroup (one: each wave a pair of its own) hold up to 64 KEYS keys each, lane l of wave w the keys
+// (64 w + l) per .. + per - 1, so indices ascend with the lanes.  The k-th largest key is found two bits at a time from
+// the top, by counting (ballots) the keys at or above the three candidates; then every lane writes the indices of its keys
+// above it, and of those equal to it as many as are still wanted.
+template <int WAVES, int KEYS>
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) k_pick_blocks(const float *__restrict__ scores, int P, int n,
+                                                                               int k, int32_t *__restrict__ blocks) {
+  __shared__ uint64_t s_count[2][WAVES];   // three counts of 21 bits
+  __shared__ uint32_t s_sum[WAVES];
+  const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+  const int p = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (p >= P) return;
-  const int per = (n + 63) / 64;
-  uint32_t key[KEYS];
+  const int per = (n + 64 * WAVES - 1) / (64 * WAVES), at0 = (64 * wave + lane) * per;
+  uint32_t key[KEYS];   // a key that is not there is 0, below every candidate but the NaNs' own, 0, which is not counted
 #pragma unroll
-  for (int i = 0; i < KEYS; ++i) {
-    const int at = lane * per + i;
-    key[i] = i < per && at < n ? score_key(scores[(int64_t)p * n + at]) : 0u;   // 0 is a NaN's key: see below
-  }
-  // Keys that are not there count like NaNs, but only at candidate 0, which is not counted.
+  for (int i = 0; i < KEYS; ++i) key[i] = i < per && at0 + i < n ? score_key(scores[(int64_t)p * n + at0 + i]) : 0u;
   uint32_t kth = 0;
-  for (int shift = 30; shift >= 0; shift -= 2) {
+  for (int shift = 30, buf = 0; shift >= 0; shift -= 2, buf ^= 1) {
     int count[3] = {0, 0, 0};
 #pragma unroll
     for (int i = 0; i < KEYS; ++i)
 #pragma unroll
       for (int d = 0; d < 3; ++d) count[d] += __popcll(__ballot(key[i] >= (kth | (uint32_t)(d + 1) << shift)));
+    if constexpr (WAVES > 1) {
+      if (lane == 0) s_count[buf][wave] = (uint64_t)count[2] << 42 | (uint64_t)count[1] << 21 | (uint64_t)count[0];
+      __syncthreads();
+      uint64_t all = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) all += s_count[buf][w];
+#pragma unroll
+      for (int d = 0; d < 3; ++d) count[d] = (int)(all >> 21 * d & 0x1fffff);
+    }
     kth |= (uint32_t)(count[2] >= k ? 3 : count[1] >= k ? 2 : count[0] >= k ? 1 : 0) << shift;
   }
   uint32_t above = 0, equal = 0;
 #pragma unroll
   for (int i = 0; i < KEYS; ++i) {
-    const bool in = i < per && lane * per + i < n;
+    const bool in = i < per && at0 + i < n;
     above += in && key[i] > kth;
     equal += in && key[i] == kth;
   }
-  const uint32_t both = above << 16 | equal;   // at most 64 KEYS each
+  const uint32_t both = above << 16 | equal;   // at most 4096 each
   uint32_t sum = both;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
     const uint32_t x = __shfl_up(sum, off, 64);
     sum += lane >= off ? x : 0u;
   }
-  const uint32_t before = sum - both, wanted = (uint32_t)k - (__shfl(sum, 63, 64) >> 16);   // of the equal ones
+  uint32_t before = sum - both, total = __shfl(sum, 63, 64);
+  if constexpr (WAVES > 1) {
+    if (lane == 63) s_sum[wave] = sum;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      before += w < wave ? s_sum[w] : 0u;
+      total += s_sum[w];
+    }
+  }
+  const uint32_t wanted = (uint32_t)k - (total >> 16);   // of the equal ones
   uint32_t seen = before & 0xffffu, at = (before >> 16) + min(seen, wanted);
   int32_t *out = blocks + (int64_t)p * k;
 #pragma unroll
   for (int i = 0; i < KEYS; ++i) {
-    const bool in = i < per && lane * per + i < n, eq = in && key[i] == kth;
-    if (in && (key[i] > kth || (eq && seen < wanted))) out[at++] = lane * per + i;
+    const bool in = i < per && at0 + i < n, eq = in && key[i] == kth;
+    if (in && (key[i] > kth || (eq && seen < wanted))) out[at++] = at0 + i;
     seen += eq;
   }
 }
@@ -511,14 +531,16 @@ hipError_t launch_select_blocks(int fmt, const QCache &c, int G, double scale, c
   const hipError_t e = fmt == ARCKV_E4M3 ? by_beta(std::integral_constant<int, ARCKV_E4M3>{})
                                          : by_beta(std::integral_constant<int, ARCKV_INT8>{});
   if (e != hipSuccess) return e;
-  // a wave per pair up to 512 blocks (256 blocks of 512 pairs 4.3 us, 512 of 256 pairs 7.2 us; 10.7 and 8.0 us in a
-  // workgroup of 16 waves), where its counts are the longer part beyond (1024 of 8 pairs 16 us, 8 us)
-  auto pick = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)((c.P + 3) / 4)), dim3(256), 0, s, scores, c.P, c.nblk, k, blocks);
+  auto pick = [&](auto kern, int per_wg, int threads) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)((c.P + per_wg - 1) / per_wg)), dim3((unsigned)threads), 0, s, scores, c.P, c.nblk,
+                       k, blocks);
     return hipGetLastError();
   };
-  if (c.nblk <= 256) return pick(k_pick_blocks<4>);
-  if (c.nblk <= 512) return pick(k_pick_blocks<8>);
+  // a wave per pair up to 256 blocks (512 pairs of 256 4.3 us, 10.7 in k_select_topt), four up to 1024 (the call for 64
+  // pairs of 1024 14.1 us, 16.1), eight up to 2048 (for 64 pairs 19.4 us, 20.1)
+  if (c.nblk <= 256) return pick(k_pick_blocks<1, 4>, 4, 256);
+  if (c.nblk <= 1024) return pick(k_pick_blocks<4, 4>, 1, 256);
+  if (c.nblk <= 2048) return pick(k_pick_blocks<8, 4>, 1, 512);
   return launch_select(scores, c.P, c.nblk, k, blocks, s);
 }
 

@@ -322,6 +322,26 @@ def decode_bench(reps=20, warmup=3):
             res[f"{label}_GBps"] = round(nbytes / (us * 1e-6) / 1e9, 1)
             res[f"{label}_hbm_frac"] = round(nbytes / (us * 1e-6) / 1e9 / PEAK_HBM_GBS, 4)
             log(f"[decode] T={T} {label}: L={L} {us:.1f} us/layer, {res[f'{label}_GBps']:.0f} GB/s")
+            if label == "compact":
+                for fmt, dtype in (("e4m3", torch.float8_e4m3fn), ("int8", torch.int8)):
+                    cache = arckv.qcache(P, L, dtype, dev, bounds=False)
+                    arckv.qcache_write(cache, K, V)
+                    for _ in range(warmup):
+                        arckv.attend_qcache(Q, cache, beta)
+                    torch.cuda.synchronize()
+                    arckv.reset_timing()
+                    arckv.set_timing(True)
+                    for _ in range(reps):
+                        arckv.attend_qcache(Q, cache, beta)
+                    torch.cuda.synchronize()
+                    arckv.set_timing(False)
+                    ms, cnt = arckv.stage_times()["attend_qcache"]
+                    us = 1e3 * ms / cnt
+                    nbytes = P * L * (d * 2 + 4) + P * -(-L // arckv.QBLOCK) * 8 + P * G * d * (2 + 4)
+                    res[f"compact_{fmt}_us"] = round(us, 2)
+                    res[f"compact_{fmt}_GBps"] = round(nbytes / (us * 1e-6) / 1e9, 1)
+                    log(f"[decode] T={T} compact {fmt}: L={L} {us:.1f} us/layer, {res[f'compact_{fmt}_GBps']:.0f} GB/s")
+                    del cache
             del K, V, Q, beta, att
             torch.cuda.empty_cache()
         res["speedup"] = round(res["full_us"] / res["compact_us"], 3)
@@ -332,7 +352,7 @@ def decode_bench(reps=20, warmup=3):
                       "with fitted bias vs full cache)", "unit": "us", "higher_is_better": False, "n_gpus": 1,
             "dtype": "bf16", "data": "synthetic (random bf16 caches and queries)",
             "config": {"workload": "decode_b64_llama8b", "pairs": P, "query_heads_per_kv": G, "rho": 0.2},
-            "kernel": "k_attend_partial<4> + k_attend_combine", "peak_hbm_GBps": PEAK_HBM_GBS, "rows": rows}
+            "kernel": "k_attend_partial<4> + k_attend_combine; k_attendq_partial<4> + k_attendq_combine", "peak_hbm_GBps": PEAK_HBM_GBS, "rows": rows}
 
 
 def dsa_bench(wl, steps=3, warmup=1):

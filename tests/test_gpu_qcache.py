@@ -262,6 +262,26 @@ S = 1 / math.sqrt(128)
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("P,G,R,F", [(256, 4, 1024, 0), (257, 4, 1024, 0), (4, 5, 1023, 1), (4, 5, 960, 33), (768, 1, 200, 70),
+                                     (200, 8, 2100, 40), (32, 16, 9000, 0), (1000, 2, 300, 0)])
+def test_attend_at_the_borders_of_the_splits(fmt, P, G, R, F):
+    """One workgroup for a pair's 16 units and one more unit, the last pair of one launch, several chunks with a tail that
+    shares a chunk with blocks, more pairs than workgroups that run at a time."""
+    print(f"attend_qcache {fmt} P={P} G={G} R={R} F={F}", flush=True)
+    g = np.random.default_rng(P + R)
+    length = g.integers(0, R + 1, P).tolist()
+    length_f = g.integers(0, F + 1, P).tolist()
+    length[0], length[-1] = R, R
+    c = filled(g, P, R, fmt, length)
+    Q = rows(g, P, G, 128)
+    K_f, V_f = (rows(g, P, F, 128), rows(g, P, F, 128)) if F else (None, None)
+    beta = torch.from_numpy(g.uniform(-3, 3, (P, R)).astype(np.float32)).cuda() if P % 2 else None
+    out = A().attend_qcache(Q, c, beta, i32(length), K_f, V_f, i32(length_f) if F else None)
+    pairs = sorted({0, 1, P // 3, P // 2, P - 2, P - 1})
+    check_attend(out, Q, c, fmt, beta, length, K_f, V_f, length_f if F else None, None, S, pairs=pairs)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("P,G,R,F", [(1, 1, 1, 0), (3, 4, 1, 1), (2, 1, 63, 0), (2, 8, 64, 0), (2, 2, 65, 31),
                                      (5, 4, 512, 0), (3, 4, 513, 257), (2, 16, 1000, 33), (2, 3, 1537, 0),
                                      (2, 13, 130, 256), (1, 4, 20000, 300), (70, 4, 700, 5)])
@@ -333,6 +353,24 @@ def test_attend_masks(fmt):
     out = A().attend_qcache(Q, c, low)
     want = np.stack([oq.q_values(np64(c.V[p]), np64(c.V_scale[p])).mean(axis=0) for p in range(P)])
     assert np.abs(np64(out) - want[:, None]).max() <= 4 * R * U * 8
+
+
+def test_attend_small_probabilities_times_large_values():
+    """A probability of e^-22 beside one of 1, its value 2^18 times the other's: what the fp16 terms keep of it shows."""
+    c = make_cache(1, 64, "e4m3")
+    K, V = torch.zeros(1, 64, 128, device="cuda"), torch.zeros(1, 64, 128, device="cuda")
+    V[0, 0] = 2.0 ** -9
+    V[0, 1] = 448
+    A().qcache_write(c, K, V)
+    assert c.V_scale[0, 0] == 1
+    beta = torch.full((1, 64), -math.inf, device="cuda")
+    beta[0, 0], beta[0, 1] = 0.0, -22.0
+    Q = rows(np.random.default_rng(0), 1, 4, 128)
+    out = np64(A().attend_qcache(Q, c, beta))
+    want = (2.0 ** -9 + 448 * math.exp(-22)) / (1 + math.exp(-22))
+    # the small one: 2^-39 of the largest probability lost, times 448; besides, float32's steps and the exponential
+    assert np.abs(out - want).max() <= 2.0 ** -39 * 448 + want * 2.0 ** -20
+    assert 448 * math.exp(-22) > 16 * (2.0 ** -39 * 448 + want * 2.0 ** -20)
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
@@ -427,7 +465,8 @@ def check_select(blocks, scores, Q, c, k, beta, length, s):
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("P,G,R,k", [(1, 1, 1, 1), (2, 4, 64, 1), (3, 8, 65, 2), (2, 16, 5000, 7), (9, 3, 4095, 64),
-                                     (2, 4, 70000, 100)])
+                                     (2, 4, 70000, 100), (5, 4, 16384, 256), (3, 4, 16385, 200), (2, 8, 65536, 1024),
+                                     (2, 4, 65537, 1), (2, 4, 131072, 64), (2, 2, 131073, 2049)])
 def test_select_blocks(fmt, P, G, R, k):
     print(f"select_blocks {fmt} P={P} G={G} R={R} k={k}", flush=True)
     g = np.random.default_rng(R)
@@ -567,6 +606,25 @@ def test_on_a_side_stream():
         out = A().attend_qcache(Q, c)
     s.synchronize()
     assert torch.equal(out, want)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with workspaces of their own (the binding's), each many chunks."""
+    g = np.random.default_rng(45)
+    cs = [filled(g, 8, 9000, "e4m3"), filled(g, 8, 9000, "int8")]
+    Q = [rows(g, 8, 4, 128), rows(g, 8, 4, 128)]
+    want = [(A().attend_qcache(q, c), A().select_blocks(q, c, 9)) for q, c in zip(Q, cs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append((A().attend_qcache(Q[i], cs[i]), A().select_blocks(Q[i], cs[i], 9)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out, (blocks, scores) in got[i]:
+            assert torch.equal(out, want[i][0]) and torch.equal(blocks, want[i][1][0]) and torch.equal(scores, want[i][1][1])
 
 
 def test_results_do_not_change_between_runs():

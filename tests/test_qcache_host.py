@@ -2,6 +2,8 @@
 (every refusal comes before any HIP call) and of the binding."""
 import ctypes
 import math
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -183,3 +185,26 @@ def test_binding_checks_shapes_types_and_devices():
     c = A.qcache(3, 130, torch.int8, device="cpu")
     assert [tuple(t.shape) for t in c] == [(3, 130, 128), (3, 130, 128), (3, 3), (3, 3), (3, 3, 2, 128)]
     assert A.qcache(1, 1, device="cpu", bounds=False).K_bounds is None
+
+
+def test_host_code_under_sanitizers():
+    """The entry points' argument checks and workspace arithmetic with AddressSanitizer and UndefinedBehaviorSanitizer on
+    the host code alone (built as tests/test_host_sanitizers.py builds the rest)."""
+    from paper_2609_36835_amd import build as B
+    from tests.test_host_sanitizers import HOST_SAN, OUT, PKG, ROOT, _kernel_objects
+    objs = _kernel_objects()
+    if not objs:
+        pytest.skip("kernel objects not built (run paper_2609_36835_amd.build first)")
+    os.makedirs(OUT, exist_ok=True)
+    hipcc, inc = B._hipcc(), ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc")]
+    host_o, drv_o, exe = (os.path.join(OUT, n) for n in ("arckv_host_q.o", "qcache_checks.o", "qcache_checks"))
+    for cmd in ([hipcc, "-std=c++17", "-fPIC", *HOST_SAN, *inc, "-c", os.path.join(PKG, "csrc", "arckv_host.cpp"), "-o", host_o],
+                [hipcc, "-std=c++17", *HOST_SAN, *inc, "-c", os.path.join(ROOT, "tests", "sanitize", "qcache_checks.cpp"),
+                 "-o", drv_o],
+                [hipcc, f"--offload-arch={B.ARCH}", *HOST_SAN, drv_o, host_o, *objs, "-o", exe]):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        assert r.returncode == 0, (" ".join(cmd), r.stderr[-4000:])
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:halt_on_error=1",
+               UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1", HIP_VISIBLE_DEVICES="")
+    r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
+    assert r.returncode == 0 and "ok: 0 failures" in r.stdout, (r.stdout[-4000:], r.stderr[-4000:])

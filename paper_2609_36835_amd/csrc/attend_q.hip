@@ -100,7 +100,7 @@ template <> struct Operand<ARCKV_INT8> {
 
 // Probabilities, times 2^kPShift, as two fp16 terms: 22 bits of the large ones, and 2^-39 of the block's largest where
 // they are small.
-constexpr float kPShift = 15.0f;
+constexpr int kPShift = 15;
 __device__ inline void split_p_f16(float p0, float p1, uint32_t &h, uint32_t &l) {
   const f32x2 x = {p0, p1};
   const f16x2 hi = __builtin_convertvector(x, f16x2);
@@ -135,11 +135,11 @@ template <int FROM> __device__ inline uint32_t from_lane(uint32_t x) {
 }
 template <int FROM> __device__ inline float from_lane(float x) { return __uint_as_float(from_lane<FROM>(__float_as_uint(x))); }
 
-// One step of a running softmax per query: turns the lane's N logits into probabilities times 2^kPShift relative to the
-// new maximum, takes them up in m and l, and returns what the earlier sums have to be multiplied by.  A query's logits lie
+// One step of a running softmax per query: turns the lane's N logits into probabilities times 2^SHIFT relative to the new
+// maximum, takes them (without 2^SHIFT) up in m and l, and returns what the earlier sums have to be multiplied by.  A query's logits lie
 // in the lanes of its column r of the four rows, and, PARTS > 1, of the columns r + 16 / PARTS, ....  -inf marks keys left
 // out; any: whether there is one that is not.
-template <int N, int PARTS> __device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any) {
+template <int N, int PARTS, int SHIFT> __device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any) {
   auto larger = [](float x, float y) { return fmaxf(x, y); };
   auto plus = [](float x, float y) { return x + y; };
   float top = sv[0];
@@ -155,14 +155,14 @@ template <int N, int PARTS> __device__ inline float softmax_step(float (&sv)[N],
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    sv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i] - ref, 1.44269504f, kPShift));
+    sv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i] - ref, 1.44269504f, (float)SHIFT));
     sum += sv[i];
   }
   if constexpr (PARTS == 4) sum += from_lane<4>(sum);
   if constexpr (PARTS >= 2) sum += from_lane<8>(sum);
   sum = over_rows(sum, plus);
   m = top;
-  l = fmaf(l, keep, sum);
+  l = fmaf(l, keep, sum * (1.0f / (1 << SHIFT)));
   return keep;
 }
 
@@ -329,7 +329,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
     if constexpr (W != kAqWide) load_keys<BETA, LINES, NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
     __builtin_amdgcn_sched_barrier(0);
     bool any;
-    const float keep = softmax_step<N, PARTS>(sv, m, l, any);
+    const float keep = softmax_step<N, PARTS, kPShift>(sv, m, l, any);
     if constexpr (BETA && FMT == ARCKV_E4M3) {
       // the probability of a token left out is zero, but zero times a NaN code is not (int8 has none)
 #pragma unroll
@@ -372,7 +372,8 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
         }
       }
     }
-    const float vscale = any ? v.scale : 0.0f;   // of a block that is left out whole it may be NaN
+    // without the probabilities' 2^kPShift; the scale of a block that is left out whole may be NaN
+    const float vscale = any ? v.scale * (1.0f / (1 << kPShift)) : 0.0f;
 #pragma unroll
     for (int dd = 0; dd < 2; ++dd) {
       f32x4 acc[4] = {};
@@ -452,7 +453,7 @@ __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, 
     if constexpr (W != kAqWide) load_tail_keys(a, next, nlive, k);
     __builtin_amdgcn_sched_barrier(0);
     bool any;
-    const float keep = softmax_step<8, 1>(sv, m, l, any);
+    const float keep = softmax_step<8, 1, 0>(sv, m, l, any);
     Frag ph, pm, pl;
     split_p(sv, ph, pm, pl);
 #pragma unroll

@@ -30,7 +30,7 @@ __device__ inline void write_block(uint8_t *codes, float *scales, uint8_t *bound
                                    int nblk, int n, int start, int end) {
   __shared__ uint32_t s_amax[4];
   __shared__ float s_bound[4][2][kHeadDim];
-  constexpr int kRow = kHeadDim * sizeof(T);
+  constexpr int kRow = kHeadDim * sizeof(T), kOutside = 1 << 30;   // an offset behind every block
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int dim = 8 * (tid & 15), r0 = tid >> 4;        // this thread's rows of the block: r0 + 16 i
   const int row0 = b * kQBlock;
@@ -43,10 +43,12 @@ __device__ inline void write_block(uint8_t *codes, float *scales, uint8_t *bound
     const __amdgpu_buffer_rsrc_t from = buffer(src + ((int64_t)p * n + row0 + kept - start) * kHeadDim, (held - kept) * kRow);
     u32x4 v[4][sizeof(T) / 2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      const int at = r0 + 16 * i < kept ? kOutside : (r0 + 16 * i - kept) * kRow + dim * (int)sizeof(T);
 #pragma unroll
-      for (int h = 0; h < (int)sizeof(T) / 2; ++h)   // a kept row's offset is negative, so out of range
-        v[i][h] = __builtin_amdgcn_raw_buffer_load_b128(from, (r0 + 16 * i - kept) * kRow + dim * (int)sizeof(T) + 16 * h, 0, kStreamed);
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+        v[i][h] = __builtin_amdgcn_raw_buffer_load_b128(from, at + 16 * h, 0, kStreamed);
+    }
     if (kept > 0) {
       const float old = scales[(int64_t)p * nblk + b];
       const __amdgpu_buffer_rsrc_t before = buffer(block, kept * kHeadDim);

@@ -355,6 +355,52 @@ def test_attend_masks(fmt):
     assert np.abs(np64(out) - want[:, None]).max() <= 4 * R * U * 8
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("R", [700, 5000])
+def test_attend_large_and_small_magnitudes(fmt, R):
+    """Values up to 2^112 and down to 2^-90, beside a tail of ordinary ones: sums neither overflow nor vanish."""
+    g = np.random.default_rng(28)
+    V = rows(g, 4, R, 128)
+    V[0] *= 2.0 ** 110
+    V[1] *= 2.0 ** -90
+    V[2, :R // 2] *= 2.0 ** 100
+    c = make_cache(4, R, fmt)
+    A().qcache_write(c, rows(g, 4, R, 128), V)
+    Q = rows(g, 4, 4, 128)
+    out = A().attend_qcache(Q, c)
+    assert out.isfinite().all()
+    check_attend(out, Q, c, fmt, None, None, None, None, None, None, S)
+    K_f, V_f = rows(g, 4, 40, 128), rows(g, 4, 40, 128)
+    check_attend(A().attend_qcache(Q, c, None, None, K_f, V_f), Q, c, fmt, None, None, K_f, V_f, None, None, S)
+
+
+def test_more_pairs_than_a_grid_row():
+    """40,000 pairs: pairs lie over two extents of a launch's grid."""
+    g = np.random.default_rng(29)
+    P, R, G = 40000, 70, 2
+    c = A().qcache(P, R, torch.int8)
+    K, V = rows(g, 1, R, 128).expand(P, R, 128).clone(), rows(g, 1, R, 128).expand(P, R, 128).clone()
+    K[32768:] *= 2
+    V[39999] *= 4
+    A().qcache_write(c, K, V)
+    k, v = A().qcache_read(c)
+    Q = rows(g, 1, G, 128).expand(P, G, 128).contiguous()
+    blocks, scores = A().select_blocks(Q, c, 1)
+    out = A().attend_qcache(Q, c)
+    small = A().qcache(3, R, torch.int8)
+    at = [0, 32768, 39999]
+    A().qcache_write(small, K[at].contiguous(), V[at].contiguous())
+    ks, vs = A().qcache_read(small)
+    bs, ss = A().select_blocks(Q[at].contiguous(), small, 1)
+    os = A().attend_qcache(Q[at].contiguous(), small)
+    ranges = [slice(0, 32768), slice(32768, 39999), slice(39999, 40000)]
+    tol = 2.0 ** -20      # other splits of the same sums
+    for i, r in enumerate(ranges):
+        for whole, one in ((k, ks), (v, vs), (scores, ss), (blocks, bs)):
+            assert torch.equal(whole[r], one[i:i + 1].expand_as(whole[r]))
+        assert (out[r] - os[i]).abs().max() <= tol * (1 + vs[i].float().abs().max())
+
+
 def test_attend_small_probabilities_times_large_values():
     """A probability of e^-22 beside one of 1, its value 2^18 times the other's: what the fp16 terms keep of it shows."""
     c = make_cache(1, 64, "e4m3")

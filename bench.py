@@ -322,26 +322,35 @@ def decode_bench(reps=20, warmup=3):
             res[f"{label}_GBps"] = round(nbytes / (us * 1e-6) / 1e9, 1)
             res[f"{label}_hbm_frac"] = round(nbytes / (us * 1e-6) / 1e9 / PEAK_HBM_GBS, 4)
             log(f"[decode] T={T} {label}: L={L} {us:.1f} us/layer, {res[f'{label}_GBps']:.0f} GB/s")
-            if label == "compact":
-                for fmt, dtype in (("e4m3", torch.float8_e4m3fn), ("int8", torch.int8)):
-                    cache = arckv.qcache(P, L, dtype, dev, bounds=False)
-                    arckv.qcache_write(cache, K, V)
+            # the same rows in 8 bits; the full cache also by its blocks, as many as hold the compact cache's rows
+            for fmt, dtype in (("e4m3", torch.float8_e4m3fn), ("int8", torch.int8)):
+                cache = arckv.qcache(P, L, dtype, dev)
+                arckv.qcache_write(cache, K, V)
+                blocks = -(-L // arckv.QBLOCK)
+                calls = {f"{label}_{fmt}": (L, lambda: arckv.attend_qcache(Q, cache, beta))}
+                if label == "full":
+                    k = -(-t // arckv.QBLOCK)
+                    calls[f"blocks_{fmt}"] = (k * arckv.QBLOCK, lambda: arckv.attend_qcache(
+                        Q, cache, blocks=arckv.select_blocks(Q, cache, k)[0]))
+                for name, (read, call) in calls.items():
                     for _ in range(warmup):
-                        arckv.attend_qcache(Q, cache, beta)
+                        call()
                     torch.cuda.synchronize()
                     arckv.reset_timing()
                     arckv.set_timing(True)
                     for _ in range(reps):
-                        arckv.attend_qcache(Q, cache, beta)
+                        call()
                     torch.cuda.synchronize()
                     arckv.set_timing(False)
-                    ms, cnt = arckv.stage_times()["attend_qcache"]
-                    us = 1e3 * ms / cnt
-                    nbytes = P * L * (d * 2 + 4) + P * -(-L // arckv.QBLOCK) * 8 + P * G * d * (2 + 4)
-                    res[f"compact_{fmt}_us"] = round(us, 2)
-                    res[f"compact_{fmt}_GBps"] = round(nbytes / (us * 1e-6) / 1e9, 1)
-                    log(f"[decode] T={T} compact {fmt}: L={L} {us:.1f} us/layer, {res[f'compact_{fmt}_GBps']:.0f} GB/s")
-                    del cache
+                    st = arckv.stage_times()
+                    us = sum(1e3 * st[n][0] / st[n][1] for n in ("attend_qcache", "select_blocks") if st[n][1])
+                    nbytes = P * (read * (2 * d + (4 if with_beta else 0)) + read // arckv.QBLOCK * 8 + G * d * (2 + 4))
+                    if name.startswith("blocks"):
+                        nbytes += P * blocks * (2 * d + 4 + 4)     # bounds and scales read, scores written
+                    res[f"{name}_us"] = round(us, 2)
+                    res[f"{name}_GBps"] = round(nbytes / (us * 1e-6) / 1e9, 1)
+                    log(f"[decode] T={T} {name}: {us:.1f} us/layer, {res[f'{name}_GBps']:.0f} GB/s")
+                del cache
             del K, V, Q, beta, att
             torch.cuda.empty_cache()
         res["speedup"] = round(res["full_us"] / res["compact_us"], 3)

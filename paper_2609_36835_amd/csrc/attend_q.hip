@@ -49,6 +49,13 @@ __device__ inline f32x4 mfma16h(bf16x8 a, bf16x8 b, f32x4 c) {   // fp16 values 
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// LDS that only one wave uses: what its lanes wrote before is there for all of them (LDS takes a wave's accesses in order,
+// so this holds back the compiler alone).
+__device__ inline void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
+
 union Frag {
   uint32_t w[4];
   bf16x8 v;
@@ -222,7 +229,7 @@ __device__ inline void put_keys(const Keys &k, u32x4 *s_k) {
     const int row = 8 * i + (lane >> 3);
     s_k[row * 8 + ((lane & 7) ^ (row >> 1 & 7))] = k.c[i / 2][i % 2];
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_exchange();
 }
 __device__ inline u32x4 get_keys(const u32x4 *s_k, int kt, int kk) {
   const int lane = threadIdx.x & 63, row = 16 * kt + (lane & 15);
@@ -243,7 +250,7 @@ __device__ inline void load_values(const AttendQ &a, int64_t pair_block, int64_t
 __device__ inline void put_queries(const bf16x8 (&qf)[4], bf16x8 *s_q) {
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks) s_q[ks * 64 + (threadIdx.x & 63)] = qf[ks];
-  __builtin_amdgcn_wave_barrier();
+  wave_exchange();
 }
 
 // The blocks first, first + W, ... below end of the list (or of the cache), a wave's share of a chunk.
@@ -304,7 +311,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
       const float bias = lane < live ? k.bias : -INFINITY;
       hidden = __ballot(lane < live && bias == -INFINITY);
       s_bias[lane] = bias;
-      __builtin_amdgcn_wave_barrier();
+      wave_exchange();
     }
 #pragma unroll
     for (int t = 0; t < N / 4; ++t) {
@@ -324,7 +331,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
         for (int j = 0; j < 4; ++j) sv[4 * t + j] = key0 + j < live ? kscale * d[j] : -INFINITY;
       }
     }
-    if constexpr (BETA) __builtin_amdgcn_wave_barrier();
+    if constexpr (BETA) wave_exchange();
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (W != kAqWide) load_keys<BETA, LINES, NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
     __builtin_amdgcn_sched_barrier(0);
@@ -518,6 +525,7 @@ __global__ void __launch_bounds__(64 * W, W == kAqW ? 3 : 4) k_attendq_partial(A
     sM[wave][r] = m;
     sL[wave][r] = l;
   }
+  wave_exchange();
   if (r < G)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

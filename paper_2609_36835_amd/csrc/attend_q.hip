@@ -331,7 +331,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
         for (int j = 0; j < 4; ++j) sv[4 * t + j] = key0 + j < live ? kscale * d[j] : -INFINITY;
       }
     }
-    if constexpr (BETA) wave_exchange();
+    if constexpr (BETA || LINES) wave_exchange();   // the next block's keys and biases take the place of what was read here
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (W != kAqWide) load_keys<BETA, LINES, NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
     __builtin_amdgcn_sched_barrier(0);

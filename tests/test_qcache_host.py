@@ -208,3 +208,30 @@ def test_host_code_under_sanitizers():
                UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1", HIP_VISIBLE_DEVICES="")
     r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
     assert r.returncode == 0 and "ok: 0 failures" in r.stdout, (r.stdout[-4000:], r.stderr[-4000:])
+
+
+@pytest.mark.parametrize("R", [130, 20000])
+def test_exact_sums_show_any_row(R):
+    """The inputs of the GPU test of attention's sums: a row left out, doubled or taken for its neighbour in the oracle
+    moves a result by more than that test allows, wherever the row lies."""
+    from tests.test_gpu_qcache_sums import exact_sums
+    g = np.random.default_rng(R)
+    K, V = (torch.from_numpy(g.integers(0, 2, (1, R, 128)).astype(np.float32)) for _ in range(2))
+    Q = torch.zeros(1, 2, 128)
+    Q[0, 1, 17] = 4096.0
+    ones = torch.ones(1, R)
+    want = exact_sums(Q, -K, V, ones, None, None, None, None)
+    for row in [0, 1, 63, 64, 65, R // 2, R - 3, R - 2]:
+        for change in ("left out", "twice", "its neighbour's value", "its neighbour's key"):
+            w, k, v = ones.clone(), -K.clone(), V.clone()
+            if change == "left out":
+                w[0, row] = 0
+            elif change == "twice":
+                w[0, row] = 2
+            elif change == "its neighbour's value":
+                v[0, row] = V[0, row + 1]
+            else:
+                k[0, row] = -K[0, row + 1]
+            got = exact_sums(Q, k, v, w, None, None, None, None)
+            seen = bool(((got - want).abs() > 2.0 ** -22 * want).any())
+            assert seen or (change == "its neighbour's key" and K[0, row, 17] == K[0, row + 1, 17]), (row, change)

@@ -142,11 +142,14 @@ template <int FROM> __device__ inline uint32_t from_lane(uint32_t x) {
 }
 template <int FROM> __device__ inline float from_lane(float x) { return __uint_as_float(from_lane<FROM>(__float_as_uint(x))); }
 
-// One step of a running softmax per query: turns the lane's N logits into probabilities times 2^SHIFT relative to the new
-// maximum, takes them (without 2^SHIFT) up in m and l, and returns what the earlier sums have to be multiplied by.  A query's logits lie
+// One step of a running softmax per query: turns the lane's N logits into probabilities times 2^SHIFT, takes them (without
+// 2^SHIFT) up in m and l, and returns what the earlier sums have to be multiplied by.  OWN: the probabilities are relative
+// to the step's own largest logit, which fp16 terms need where it lies far below the largest of all, and `now` is what this
+// step's sums have to be multiplied by; else they are relative to the new maximum and `now` is not used.  A query's logits lie
 // in the lanes of its column r of the four rows, and, PARTS > 1, of the columns r + 16 / PARTS, ....  -inf marks keys left
 // out; any: whether there is one that is not.
-template <int N, int PARTS, int SHIFT> __device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any) {
+template <int N, int PARTS, int SHIFT, bool OWN>
+__device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any, float &now) {
   auto larger = [](float x, float y) { return fmaxf(x, y); };
   auto plus = [](float x, float y) { return x + y; };
   float top = sv[0];
@@ -156,9 +159,10 @@ template <int N, int PARTS, int SHIFT> __device__ inline float softmax_step(floa
   if constexpr (PARTS >= 2) top = fmaxf(top, from_lane<8>(top));
   top = over_rows(top, larger);
   any = top != -INFINITY;
+  const float own = any ? top : 0.0f;
   top = fmaxf(top, m);
-  const float ref = top == -INFINITY ? 0.0f : top;
-  const float keep = __builtin_amdgcn_exp2f((m - ref) * 1.44269504f);
+  const float all = top == -INFINITY ? 0.0f : top, ref = OWN ? own : all;
+  const float keep = __builtin_amdgcn_exp2f((m - all) * 1.44269504f);
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -168,6 +172,10 @@ template <int N, int PARTS, int SHIFT> __device__ inline float softmax_step(floa
   if constexpr (PARTS == 4) sum += from_lane<4>(sum);
   if constexpr (PARTS >= 2) sum += from_lane<8>(sum);
   sum = over_rows(sum, plus);
+  if constexpr (OWN) {
+    now = any ? __builtin_amdgcn_exp2f((own - all) * 1.44269504f) : 0.0f;
+    sum *= now;
+  }
   m = top;
   l = fmaf(l, keep, sum * (1.0f / (1 << SHIFT)));
   return keep;
@@ -336,7 +344,8 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
     if constexpr (W != kAqWide) load_keys<BETA, LINES, NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, k);
     __builtin_amdgcn_sched_barrier(0);
     bool any;
-    const float keep = softmax_step<N, PARTS, kPShift>(sv, m, l, any);
+    float now;
+    const float keep = softmax_step<N, PARTS, kPShift, true>(sv, m, l, any, now);
     if constexpr (BETA && FMT == ARCKV_E4M3) {
       // the probability of a token left out is zero, but zero times a NaN code is not (int8 has none)
 #pragma unroll
@@ -380,7 +389,7 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
       }
     }
     // without the probabilities' 2^kPShift; the scale of a block that is left out whole may be NaN
-    const float vscale = any ? v.scale * (1.0f / (1 << kPShift)) : 0.0f;
+    const float vscale = any ? v.scale * (1.0f / (1 << kPShift)) * now : 0.0f;
 #pragma unroll
     for (int dd = 0; dd < 2; ++dd) {
       f32x4 acc[4] = {};
@@ -460,7 +469,8 @@ __device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, 
     if constexpr (W != kAqWide) load_tail_keys(a, next, nlive, k);
     __builtin_amdgcn_sched_barrier(0);
     bool any;
-    const float keep = softmax_step<8, 1, 0>(sv, m, l, any);
+    float now;
+    const float keep = softmax_step<8, 1, 0, false>(sv, m, l, any, now);
     Frag ph, pm, pl;
     split_p(sv, ph, pm, pl);
 #pragma unroll

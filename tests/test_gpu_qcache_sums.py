@@ -4,6 +4,11 @@ Exact sums: keys, queries and biases are chosen so that a logit is the largest o
 so a probability is 1 / n or 0; values are 0 and 1, stored without error.  The kernels' sums are then whole numbers, the
 factors that join them 1 or 0, and what is left is one division: 2^-24 of the result, 2^-22 allowed.  A row that is lost,
 read twice or read in another's place changes a sum by at least 1 of n <= 2^19.
+
+Far logits: a block whose logits lie D below another's, its values larger by as much.  u = 2^-24; the logits are exact; an
+exponential's argument is off by the steps of its subtraction, of its product and of log2 e, D u each, the exponential by 4u; 64
+products are summed at 2u each (the accumulator may truncate), as are the probabilities, and each is halved into two
+terms (4u); joining, scaling and dividing add 32u: (3 D + 320) u sum_j p_j |v_j|.
 """
 import math
 
@@ -11,7 +16,8 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_qcache import A, DT
+from oracle import qcache as oq
+from tests.test_gpu_qcache import A, DT, U, np64
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +95,40 @@ def test_every_row_once(fmt, form, P, G, R, F):
     want = exact_sums(Q, K, V, weight, bias, K_f, V_f, weight_f)
     bad = (out - want).abs() > 2.0 ** -22 * want
     assert not bad.any() and out.isfinite().all(), bad.nonzero()[:5].tolist()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("by", ["bias", "keys"])
+@pytest.mark.parametrize("D", [20, 28, 30, 60])
+@pytest.mark.parametrize("P", [3, 500])
+def test_far_logits_with_large_values(fmt, by, D, P):
+    """Two blocks that one wave takes in turn (500 pairs) or two waves do (3 pairs), in both orders: the one with the small
+    probabilities decides the result."""
+    print(f"attend_qcache {fmt} {by} D={D} P={P}", flush=True)
+    g = np.random.default_rng(D)
+    R, G = 512, 4
+    K = torch.zeros(P, R, 128, device="cuda")
+    bias = torch.full((P, R), -math.inf, device="cuda")
+    V = torch.from_numpy(g.standard_normal((1, R, 128)).astype(np.float32)).cuda().repeat(P, 1, 1)
+    K[:, :, 5] = -40.0                                               # 40 D below: nothing
+    for p in range(2):
+        near, far = (0, 256) if p == 0 else (256, 0)
+        K[p::2, near:near + 64, 5] = 0.0
+        K[p::2, far:far + 64, 5] = -1.0
+        bias[p::2, near:near + 64] = 0.0
+        bias[p::2, far:far + 64] = -float(D)
+        V[p::2, far:far + 64] *= 2.0 ** (1.5 * D + 15)
+    if by == "bias":
+        K.zero_()
+    else:
+        bias = None
+    Q = torch.zeros(P, G, 128, device="cuda", dtype=torch.bfloat16)
+    Q[:, :, 5] = float(D)
+    c = A().qcache(P, R, DT[fmt])
+    A().qcache_write(c, K, V)
+    out = np64(A().attend_qcache(Q, c, bias, scale=1.0))
+    for p in sorted({0, 1, 2, P // 2, P - 1}):
+        k, v = oq.q_values(np64(c.K[p]), np64(c.K_scale[p])), oq.q_values(np64(c.V[p]), np64(c.V_scale[p]))
+        ref, mass = oq.q_attend(np64(Q[p]), k, v, None if bias is None else np64(bias[p]), None, None, 1.0)
+        assert np.abs(ref).max() > 1e3                               # the far block's, not the near one's
+        assert (np.abs(out[p] - ref) <= (3 * D + 320) * U * mass).all(), (p, float((np.abs(out[p] - ref) / mass).max()))

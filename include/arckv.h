@@ -376,8 +376,12 @@ arckv_status arckv_assign_stats(const arckv_problem *prob, int32_t t, const void
  *   the stored value is scale * code.
  * Scales are powers of two, so the codes do not depend on how they are computed,
  * a stored value is exact in bfloat16, and storing it again changes nothing.
- * An error is at most half a step: 2^-4 of the value's magnitude (2^-10 scale for the
- * smallest) in e4m3, scale / 2 in int8, where a scale is below A / 63.5.  Keys
+ * An error is at most half a step where a block is written once: 2^-4 of the value's
+ * magnitude (2^-10 scale for the smallest) in e4m3, scale / 2 in int8, where a scale
+ * is below A / 63.5 (or 2^-100).  A row kept in a block whose scale grows is rounded again
+ * (a prompt's last block, every block of single tokens).  The halves add up, but to
+ * less than a step of the largest scale that the block has had since: scale in int8;
+ * 2^-9 scale in e4m3, where values of 2^-6 scale and more keep their 2^-4.  Keys
  * with outlier channels lose less in e4m3, values of one magnitude less in int8.
  * A block that holds a non-finite number has a NaN scale and reads as NaN.
  * (The largest magnitudes, above 2^127, may round to infinity.)

@@ -709,3 +709,28 @@ def test_offsets_past_32_bits():
     out = A().attend_qcache(Q, c, None, full, blocks=blocks)
     every = torch.arange(4, dtype=torch.int32, device="cuda").repeat(2, 1)
     assert torch.equal(out[P - 2:], A().attend_qcache(Q[P - 2:].contiguous(), small, blocks=every))
+
+
+@pytest.mark.parametrize("fmt,growth", [("int8", 1.02), ("int8", 1.1), ("e4m3", 1.1), ("e4m3", 1.4)])
+def test_single_tokens_stay_within_a_step(fmt, growth):
+    """Blocks written row by row, so that kept rows are rounded again whenever the scale grows: less than a step of the
+    largest scale since in int8; in e4m3 2^-4 of the value from 2^-6 scale on, less than 2^-9 scale below."""
+    g = np.random.default_rng(11)
+    P, R = 3, 128
+    x = rows(g, P, R, 128) * torch.tensor(growth).pow(torch.arange(R) % 64).cuda()[None, :, None]
+    x = x.to(torch.bfloat16)
+    c = make_cache(P, R, fmt)
+    s = torch.zeros(P, R, 1, device="cuda", dtype=torch.float64)       # the largest scale since the row was written
+    for i in range(R):
+        A().qcache_write(c, x[:, i:i + 1].contiguous(), -x[:, i:i + 1].contiguous(), i32([i] * P))
+        since = s[:, i // 64 * 64:i + 1]
+        since.copy_(torch.maximum(since, c.K_scale[:, i // 64, None, None].double()))
+    k, v = A().qcache_read(c, dtype=torch.float32)
+    assert torch.equal(k, -v)
+    err, x = (k.double() - x.double()).abs(), x.double().abs()
+    half = s / 2 if fmt == "int8" else torch.maximum(x * 2.0 ** -4, s * 2.0 ** -10)
+    if fmt == "int8":
+        assert (err < s).all()
+    else:
+        assert torch.where(x >= 2.0 ** -6 * s, err <= 2.0 ** -4 * x, err < 2.0 ** -9 * s).all()
+    assert (err > half).any()                            # more than a block written once is off by

@@ -235,3 +235,36 @@ def test_exact_sums_show_any_row(R):
             got = exact_sums(Q, k, v, w, None, None, None, None)
             seen = bool(((got - want).abs() > 2.0 ** -22 * want).any())
             assert seen or (change == "its neighbour's key" and K[0, row, 17] == K[0, row + 1, 17]), (row, change)
+
+
+def step_by_step(fmt, growth):
+    """64 rows, each `growth` times the one before, written one at a time: rows, stored values, and for each row the
+    largest scale since it was written."""
+    g = np.random.default_rng(4)
+    x = g.standard_normal((64, 16)) * np.exp(math.log(growth) * np.arange(64))[:, None]
+    codes, scales, largest = np.zeros((64, 16)), np.full(1, 2.0 ** -100), np.zeros((64, 1))
+    for i in range(64):
+        oq.q_write(codes, scales, x[i:i + 1], i, fmt)
+        largest[:i + 1] = np.maximum(largest[:i + 1], scales[0])
+    return x, oq.q_values(codes, scales), largest
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("growth", [1.0, 1.02, 1.1, 1.4])
+def test_rows_kept_in_a_growing_block_stay_within_a_step(fmt, growth):
+    """Each doubling of the scale can add half a step of the new one: s / 2 + s / 4 + ... < s in all.  In e4m3 only values
+    below 2^-6 scale are rounded again, in steps of 2^-9 scale."""
+    x, v, s = step_by_step(fmt, growth)
+    err = np.abs(v - x)
+    if fmt == "int8":
+        assert (err < s).all()
+    else:
+        large = np.abs(x) >= 2.0 ** -6 * s
+        assert (err[large] <= 2.0 ** -4 * np.abs(x[large])).all() and (err < 2.0 ** -9 * s)[~large].all()
+
+
+@pytest.mark.parametrize("fmt,growth", [("int8", 1.02), ("e4m3", 1.1)])
+def test_rows_kept_in_a_growing_block_pass_half_a_step(fmt, growth):
+    x, v, s = step_by_step(fmt, growth)
+    half = s / 2 if fmt == "int8" else np.maximum(np.abs(x) * 2.0 ** -4, s * 2.0 ** -10)
+    assert (np.abs(v - x) > half).any()

@@ -383,7 +383,9 @@ arckv_status arckv_assign_stats(const arckv_problem *prob, int32_t t, const void
  * less than a step of the largest scale that the block has had since: scale in int8;
  * 2^-9 scale in e4m3, where values of 2^-6 scale and more keep their 2^-4.  Keys
  * with outlier channels lose less in e4m3, values of one magnitude less in int8.
- * A block that holds a non-finite number has a NaN scale and reads as NaN.
+ * A block that holds a non-finite number has a NaN scale and reads as NaN, and so do
+ * rows kept in it when later ones are replaced: writing the block from its first row
+ * on makes it whole again.
  * (The largest magnitudes, above 2^127, may round to infinity.)
  *
  * The caller owns every array and the number of rows that each pair holds

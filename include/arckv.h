@@ -430,11 +430,14 @@ arckv_status arckv_qcache_read(const arckv_qcache *c, int32_t first, int32_t n, 
 /* The k blocks of each pair that its G query rows can give the largest logits to.
  * With lo, hi the block's bounds times its scale, the block's score is
  *   max_g [ s sum_d max(q_gd lo_d, q_gd hi_d) ] + max_j beta_j  (j over the block's rows),
- * which no logit of a stored key of the block exceeds; -inf for a block that holds
- * no row, or none with a bias above -inf; NaN for one with a NaN scale or a query
- * with a non-finite channel.  The sum is exact for channels down to 2^-24 of a query
- * row's largest (what smaller ones have below 2^-32 of it is cut off), and the
- * score rounded once to float32, so the choice does not hang on the order of sums.
+ * which no logit of a stored key of the block exceeds by more than the roundings
+ * below; -inf for a block that holds no row, or none with a bias above -inf; NaN for
+ * one with a NaN scale or a query with a non-finite channel.  The sum over channels
+ * is formed in float64 from exact parts, in one order whatever the call, and the
+ * score rounded to float32 at the end: to the nearest, by up to 2^-24 of it either way.
+ * Query channels of at least 2^-24 of the row's largest magnitude A enter whole; of
+ * smaller ones what lies below 2^-31 A may be cut off, which takes at most
+ * 2^-24 s A max_d(|lo_d|, |hi_d|) from a score.
  *   Q      [P][G][128] bfloat16, 16-byte aligned, G in 1..16;
  *   beta   [P][rows] float32, or NULL;
  *   length [P] device array of rows held (clipped to [0, rows]), or NULL: all;

@@ -229,9 +229,11 @@ hipError_t launch_qcache_read(int fmt, int dtype, const QCache &c, int first, in
 
 // ---------------------------------------------------------------- block scores
 // s_b = max_g [ scale * kappa_b * sum_d max(q_gd lo_bd, q_gd hi_bd) ] (+ max beta of
-// the block's tokens): no logit of the block's stored keys exceeds it.  The
-// order of blocks decides what a step attends to, so it must not hang on the
-// rounding of a sum: the sums are exact, and rounded once to float32.
+// the block's tokens): no logit of the block's stored keys exceeds it but by its
+// roundings.  The order of blocks decides what a step attends to, so it must not
+// hang on the order of a sum: the parts below are exact sums, four of them a
+// query row, and meet in float64 (exactly for int8, 48 bits; 57 in e4m3) before
+// the one rounding to float32.
 //
 // The sum is (q+ . hi) + (q- . lo) with the positive and negative parts of q, a
 // product of matrices, and MFMA's float32 sums are exact if every product is a
@@ -242,7 +244,7 @@ hipError_t launch_qcache_read(int fmt, int dtype, const QCache &c, int first, in
 // 2^(E - 32)), four query rows times four planes filling the 16 columns, and
 // codes as they are (int8: |c| <= 127, units of 1) or as nearest whole numbers
 // and the rests in units of 2^-9 (e4m3: both at most 448 and 256 units): at
-// most 448 * 255 * 128 < 2^24.  The planes' sums meet in float64.
+// most 448 * 255 * 128 < 2^24.
 constexpr int kBsTile = 16;   // blocks per wave and step
 
 // max and sum over lanes of a 16-lane row by DPP moves of a double's halves

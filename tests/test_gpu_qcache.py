@@ -734,3 +734,32 @@ def test_single_tokens_stay_within_a_step(fmt, growth):
     else:
         assert torch.where(x >= 2.0 ** -6 * s, err <= 2.0 ** -4 * x, err < 2.0 ** -9 * s).all()
     assert (err > half).any()                            # more than a block written once is off by
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_block_scores_bound_the_logits_up_to_their_roundings(fmt):
+    """No logit exceeds its block's score by more than half a step of float32 and what is cut off small channels: 2^-24 of
+    s times the query's largest magnitude times the block's largest key.  Each can put the score below a logit."""
+    g = np.random.default_rng(36)
+    P, R, G = 4, 640, 4
+    K = rows(g, P, R, 128)
+    Q = rows(g, P, G, 128)
+    K[1:3] = K[1:3].abs()
+    K[1:3, :, 0] = 0
+    Q[1, :, 1:] = 2.0 ** -33 * Q[1, :, 1:].abs().clamp(0.25, 2)         # beside channel 0, where the keys are 0
+    Q[1:3, :, 0] = 1.0
+    Q[2, :, 1:] = 2.0 ** -20 * Q[2, :, 1:].abs()
+    K[3] = K[3, :1]                                                      # blocks of one key: the bound is its logit
+    c = make_cache(P, R, fmt)
+    A().qcache_write(c, K, K)
+    _, scores = A().select_blocks(Q, c, 1)
+    sc = np64(scores)
+    over = np.zeros(P, bool)
+    for p in range(P):
+        k = oq.q_values(np64(c.K[p]), np64(c.K_scale[p]))
+        logit = (S * np64(Q[p]) @ k.T).max(axis=0).reshape(-1, 64).max(axis=1)
+        reach = np.abs(k).reshape(-1, 64 * 128).max(axis=1)
+        slack = 1.001 * U * np.abs(sc[p]) + 2.0 ** -24 * S * np.abs(np64(Q[p])).max() * reach
+        assert (logit <= sc[p] + slack).all(), p
+        over[p] = (logit > sc[p]).any()
+    assert over[1] and (sc[1] == 0).all()

@@ -479,6 +479,14 @@ def _qformat(dtype: torch.dtype) -> int:
     raise TypeError(f"unsupported cache dtype {dtype}")
 
 
+def _int32(x, what: str) -> int:
+    """x as the C argument `what`; ctypes would take it modulo 2^32."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{what}: {x} does not fit 32 bits")
+    return x
+
+
 def _qptr(x: Optional[torch.Tensor], shape, dtype: torch.dtype, device: int, what: str):
     """Pointer of a tensor that has to have this shape and type and live on the current device."""
     if x is None:
@@ -523,11 +531,12 @@ def qcache_write(cache, K, V, start=None, count=None) -> None:
 def qcache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bfloat16, length=None):
     """arckv_qcache_read: rows first .. first + n - 1 as (K, V) [P][n][128] of dtype (f32 or bf16); zeros from row
     length[p] (int32 [P]) on."""
+    first, n = _int32(first, "first"), n if n is None else _int32(n, "n")
     st, P, rows, dev = _qcache(cache)
-    n = rows - int(first) if n is None else int(n)
+    n = rows - first if n is None else n
     code = _dtype_code(dtype)
-    K, V = torch.empty(2, P, max(n, 0), 128, dtype=dtype, device=cache[0].device)
-    _check(lib().arckv_qcache_read(ctypes.byref(st), int(first), n, code, _qptr(length, (P,), torch.int32, dev, "length"),
+    K, V = torch.empty(2, P, min(max(n, 0), rows), 128, dtype=dtype, device=cache[0].device)
+    _check(lib().arckv_qcache_read(ctypes.byref(st), first, n, code, _qptr(length, (P,), torch.int32, dev, "length"),
                                    K.data_ptr(), V.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
            "arckv_qcache_read")
     return K, V
@@ -536,14 +545,15 @@ def qcache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bflo
 def select_blocks(Q, cache, k: int, beta=None, length=None, scale=None):
     """arckv_select_blocks: (blocks [P][k] int32 ascending, scores [P][ceil(rows / 64)]) for queries Q [P][G][128]
     bf16, beta [P][rows] f32 or None, length [P] int32 or None."""
+    k = _int32(k, "k")
     st, P, rows, dev = _qcache(cache)
     G, n = Q.shape[1], -(-rows // QBLOCK)
     scores = torch.empty(P, n, dtype=torch.float32, device=Q.device)
-    blocks = torch.empty(P, max(int(k), 0), dtype=torch.int32, device=Q.device)
+    blocks = torch.empty(P, min(max(k, 0), n), dtype=torch.int32, device=Q.device)
     _check(lib().arckv_select_blocks(ctypes.byref(st), G, float(scale) if scale else 0.0,
                                      _qptr(Q, (P, G, 128), torch.bfloat16, dev, "Q"),
                                      _qptr(beta, (P, rows), torch.float32, dev, "beta"),
-                                     _qptr(length, (P,), torch.int32, dev, "length"), int(k), scores.data_ptr(),
+                                     _qptr(length, (P,), torch.int32, dev, "length"), k, scores.data_ptr(),
                                      blocks.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
            "arckv_select_blocks")
     return blocks, scores
@@ -551,8 +561,8 @@ def select_blocks(Q, cache, k: int, beta=None, length=None, scale=None):
 
 def attend_qcache_workspace_size(P: int, rows: int, G: int, nsel: int = 0, F: int = 0) -> int:
     out = ctypes.c_size_t()
-    _check(lib().arckv_attend_qcache_workspace_size(int(P), int(rows), int(G), int(nsel), int(F), ctypes.byref(out)),
-           "arckv_attend_qcache_workspace_size")
+    args = [_int32(x, what) for x, what in ((P, "P"), (rows, "rows"), (G, "G"), (nsel, "nsel"), (F, "F"))]
+    _check(lib().arckv_attend_qcache_workspace_size(*args, ctypes.byref(out)), "arckv_attend_qcache_workspace_size")
     return out.value
 
 
@@ -565,7 +575,7 @@ def attend_qcache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f
     st, P, rows, dev = _qcache(cache)
     G = Q.shape[1]
     F = K_f.shape[1] if K_f is not None else 0
-    nsel = blocks.shape[1] if blocks is not None else 0
+    nsel = _int32(blocks.shape[1], "blocks") if blocks is not None else 0
     if blocks is not None and nsel == 0:
         raise ValueError("blocks: an empty list")
     row = (P,)

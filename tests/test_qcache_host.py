@@ -268,3 +268,21 @@ def test_rows_kept_in_a_growing_block_pass_half_a_step(fmt, growth):
     x, v, s = step_by_step(fmt, growth)
     half = s / 2 if fmt == "int8" else np.maximum(np.abs(x) * 2.0 ** -4, s * 2.0 ** -10)
     assert (np.abs(v - x) > half).any()
+
+
+def test_binding_refuses_what_32_bits_do_not_hold():
+    """A C argument of 32 bits takes a larger number modulo 2^32: row 2^32 would be row 0."""
+    c = A.qcache(2, 100, device="cpu")
+    Q = torch.zeros(2, 4, 128, dtype=torch.bfloat16)
+    for big in (1 << 31, 1 << 32, (1 << 32) + 1, -(1 << 31) - 1):
+        with pytest.raises(ValueError, match="first"):
+            A.qcache_read(c, big, 4)
+        with pytest.raises(ValueError, match="n:"):
+            A.qcache_read(c, 0, big)
+        with pytest.raises(ValueError, match="k:"):
+            A.select_blocks(Q, c, big)
+        for i in range(5):
+            args = [2, 100, 4, 0, 0]
+            args[i] = big
+            with pytest.raises(ValueError, match="32 bits"):
+                A.attend_qcache_workspace_size(*args)

@@ -1096,7 +1096,7 @@ arckv_status arckv_attend_qcache(const arckv_qcache *c, int32_t G, int32_t nsel,
   const float s = scale > 0.0f ? scale : 1.0f / sqrtf((float)kHeadDimH);
   STAGE(ST_ATTEND_QCACHE,
         launch_attendq(c->format, make_qcache(c), G, F, s, Q, beta, length, blocks, nsel, F > 0 ? K_f : nullptr,
-                       F > 0 ? V_f : nullptr, length_f, (float *)ws, (float *)((char *)ws + ml), out, stream));
+                       F > 0 ? V_f : nullptr, length_f, (float *)ws, need ? (float *)((char *)ws + ml) : nullptr, out, stream));
   return ARCKV_OK;
 }
 

@@ -286,3 +286,25 @@ def test_binding_refuses_what_32_bits_do_not_hold():
             args[i] = big
             with pytest.raises(ValueError, match="32 bits"):
                 A.attend_qcache_workspace_size(*args)
+
+
+@needs_no_gpu
+def test_no_workspace_under_sanitizers():
+    """A call that needs no workspace forms no address from the null pointer in its place."""
+    from paper_2609_36835_amd import build as B
+    from tests.test_host_sanitizers import HOST_SAN, OUT, PKG, ROOT, _kernel_objects
+    objs = _kernel_objects()
+    if not objs:
+        pytest.skip("kernel objects not built (run paper_2609_36835_amd.build first)")
+    os.makedirs(OUT, exist_ok=True)
+    hipcc, inc = B._hipcc(), ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc")]
+    host_o, drv_o, exe = (os.path.join(OUT, n) for n in ("arckv_host_n.o", "qcache_no_workspace.o", "qcache_no_workspace"))
+    for cmd in ([hipcc, "-std=c++17", "-fPIC", *HOST_SAN, *inc, "-c", os.path.join(PKG, "csrc", "arckv_host.cpp"), "-o", host_o],
+                [hipcc, "-std=c++17", *HOST_SAN, *inc, "-c",
+                 os.path.join(ROOT, "tests", "sanitize", "qcache_no_workspace.cpp"), "-o", drv_o],
+                [hipcc, f"--offload-arch={B.ARCH}", *HOST_SAN, drv_o, host_o, *objs, "-o", exe]):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        assert r.returncode == 0, (" ".join(cmd), r.stderr[-4000:])
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:halt_on_error=1", UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
+    assert r.returncode == 0 and "ok: size 0, 0 bytes" in r.stdout, (r.stdout[-4000:], r.stderr[-4000:])

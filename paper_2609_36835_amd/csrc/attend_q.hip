@@ -416,7 +416,6 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
     if constexpr (W == kAqWide) return;   // its only block
     load_values<NTV>(a, pb + nb, pr + (int64_t)nb * kQBlock, nlive, v);
     __builtin_amdgcn_sched_barrier(0);
-    b = nb;
     live = nlive;
   }
 }

@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) k_pick_blocks(c
     above += in && key[i] > kth;
     equal += in && key[i] == kth;
   }
-  const uint32_t both = above << 16 | equal;   // at most 4096 each
+  const uint32_t both = above << 16 | equal;   // at most 2048 each
   uint32_t sum = both;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {

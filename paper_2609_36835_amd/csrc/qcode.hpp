@@ -14,10 +14,7 @@ template <int FMT> struct QCode;
 template <> struct QCode<ARCKV_E4M3> {
   static constexpr int kExpBits = 8;                    // 448 = 1.75 * 2^8
   static constexpr uint32_t kTopMantissa = 0x600000u;   // of 1.75
-  // two values, rounded to nearest even, in the low half of the result
-  __device__ static inline uint32_t pack2(float a, float b) {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xffffu;
-  }
+  // rounded to nearest even
   __device__ static inline uint32_t pack4(float a, float b, float c, float d) {
     const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);

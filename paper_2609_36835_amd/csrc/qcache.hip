@@ -418,8 +418,8 @@ __device__ inline float tile_scores(const QCache &c, const TileBounds &t, int p,
   return there ? (float)score : -INFINITY;
 }
 
-// A wave per tile of 16 blocks and step, whose bounds are on their way while the workgroup makes its planes or the wave
-// is at the tile before.
+// A wave per tile of 16 blocks and step.  The next tile's bounds are asked for before this one's scores, but do not stay in
+// flight: loads return in order, and the wait for this tile's scales (the queries', for the first tile) is for them too.
 template <int FMT, int CT, bool BETA>
 __global__ void __launch_bounds__(256) k_block_scores(QCache c, int G, double scale, const bf16 *__restrict__ Q,
                                                       const float *__restrict__ beta,
@@ -447,7 +447,8 @@ __global__ void __launch_bounds__(256) k_block_scores(QCache c, int G, double sc
 // number.  WAVES of a workgroup (one: each wave a pair of its own) hold up to 64 KEYS keys each, lane l of wave w the keys
 // (64 w + l) per .. + per - 1, so indices ascend with the lanes.  The k-th largest key is found two bits at a time from
 // the top, by counting (ballots) the keys at or above the three candidates; then every lane writes the indices of its keys
-// above it, and of those equal to it as many as are still wanted.
+// above it, and of those equal to it as many as are still wanted.  Each key's load stands under its own condition and is waited
+// for before the next.
 template <int WAVES, int KEYS>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) k_pick_blocks(const float *__restrict__ scores, int P, int n,
                                                                                int k, int32_t *__restrict__ blocks) {

@@ -306,11 +306,11 @@ def run(s):
                                 transpose=case["transpose"], factor=s["factor"], out=s["q_out"], out_other=s["k_out"])
         cache = s["cache"]
         if kind == "write":
-            arckv.q4cache_write(cache, s["K"], s["V"], s["start"], s["count"])
+            arckv.ncache_write(cache, s["K"], s["V"], s["start"], s["count"])
             return cache
         if kind == "read":
-            return arckv.q4cache_read(cache, case["first"], case["n"], _dtype(case), s["length"])
-        return arckv.attend_q4cache(s["Q"], cache, s["beta"], s["length"], s["K_f"], s["V_f"], s["length_f"])
+            return arckv.ncache_read(cache, case["first"], case["n"], _dtype(case), s["length"])
+        return arckv.attend_ncache(s["Q"], cache, s["beta"], s["length"], s["K_f"], s["V_f"], s["length_f"])
     if kind == "rotary":
         # angles in 64 bits: in 32 those of far positions are off by a thousandth
         angle = s["positions"].double()[:, None] * s["freq"]

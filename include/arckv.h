@@ -478,6 +478,135 @@ arckv_status arckv_attend_qcache(const arckv_qcache *c, int32_t G, int32_t nsel,
                                  const void *V_f, const int32_t *length_f, float *out, void *ws, size_t ws_bytes,
                                  hipStream_t stream);
 
+/* ------------------------------------------------------------------ 4-bit cache
+ * Keys and values of P pairs in 4 bits (two codes, nibbles, to a byte: "ncache"), every row on its own: 128 codes of a row
+ * in 64 bytes and a scale for each group of 32 consecutive channels in a byte, 68
+ * bytes against the 256 of bfloat16 (136 a token with its value).
+ *   code   e2m1: sign, two exponent bits, one mantissa bit; the magnitudes 0, 0.5,
+ *          1, 1.5, 2, 3, 4, 6 in the order of the codes 0..7, negatives 8..15.
+ *          Channel 2 j is the low half of byte j of the row, channel 2 j + 1 the high.
+ *   scale  2^e, e the smallest whole number in [-100, 125] with A <= 6 * 2^e (125
+ *          where there is none), A the largest magnitude of the group; held as e + 127.
+ *   code = x / scale rounded to the nearest code, ties to even (an even code); the
+ *   stored value is scale * code.  A zero keeps its sign.
+ * Scales are powers of two, so the codes do not depend on how they are computed, a
+ * stored value is exact in bfloat16, and storing it again gives the same values.  An
+ * error is at most half a step: a quarter of the value's magnitude from one scale
+ * on, a quarter of the scale below it (magnitudes above 7 * 2^125 become 6 * 2^125).
+ * A group with a non-finite number has the scale byte 255 and codes of 0, and reads
+ * as NaN.  Rows do not depend on each other: a write changes the rows it
+ * writes and nothing else.
+ *
+ * The caller owns the arrays and the number of rows that each pair holds.  Rows
+ * behind a pair's length are never read and need not be initialised. */
+typedef struct {
+  int32_t P;              /* pairs, 1..2^20 */
+  int32_t rows;           /* rows that a pair has room for, 1..2^26 */
+  int32_t d;              /* head dimension; must be 128 */
+  void *K, *V;            /* codes [P][rows][64] bytes, 16-byte aligned */
+  void *K_scale, *V_scale;  /* [P][rows][4] bytes, 4-byte aligned */
+} arckv_ncache;
+
+/* Write n rows of keys and values, [P][n][128] float32 or bfloat16 (dtype; 16-byte
+ * aligned), into the cache, as arckv_qcache_write does:
+ *   start [P] device array: the first row to write, or NULL for 0 (clipped to [0, rows]);
+ *   count [P] device array: how many of the pair's n source rows to write, or NULL
+ *         for all (clipped to [0, n]); rows that would lie past the cache's end are dropped.
+ * Needs 1 <= n <= rows.  No workspace, no synchronisation. */
+arckv_status arckv_ncache_write(const arckv_ncache *c, int32_t n, int32_t dtype, const void *K, const void *V,
+                                const int32_t *start, const int32_t *count, hipStream_t stream);
+
+/* Read rows first .. first + n - 1 of every pair, as float32 or bfloat16 (dtype;
+ * both exact), into K and V [P][n][128], 16-byte aligned.  Rows at or past the
+ * pair's length ([P] device array, or NULL: all rows are held) come back as
+ * zeros.  Needs first >= 0, n >= 1, first + n <= rows. */
+arckv_status arckv_ncache_read(const arckv_ncache *c, int32_t first, int32_t n, int32_t dtype, const int32_t *length,
+                               void *K, void *V, hipStream_t stream);
+
+/* Decode attention over the 4-bit cache followed by an optional uncompressed block:
+ * for each pair and each of its G query rows,
+ *   out = softmax([s q K^T + beta, s q K_f^T]) [V; V_f]
+ * with K, V the stored values: arckv_attend_qcache's counterpart without lists of
+ * blocks; over (C_k, beta, C_v) written by arckv_ncache_write it is the consumer of
+ * a compaction in 4 bits.
+ *   Q        [P][G][128] bfloat16, G in 1..16.
+ *   beta     [P][rows] float32, or NULL for zero bias.  A row with beta = -inf is
+ *            left out, whatever its key and value hold.
+ *   length   [P] device array of rows held (clipped to [0, rows]), or NULL: all.
+ *   K_f, V_f [P][F][128] bfloat16 (may be NULL when F = 0).
+ *   length_f [P] device array of rows held in K_f, V_f (clipped to [0, F]), or NULL: F.
+ *   out      [P][G][128] float32; zeros for a pair without any row to attend to, NaN
+ *            for a query row with a non-finite channel where there is one.
+ * Tensors 16-byte aligned (per-pair int32 and float32 arrays by element).  Workspace:
+ * arckv_attend_ncache_workspace_size bytes; 0 where a pair's rows are one
+ * workgroup's work, ws may then be NULL.  Reads every code once. */
+arckv_status arckv_attend_ncache_workspace_size(int32_t P, int32_t rows, int32_t G, int32_t F, size_t *bytes);
+arckv_status arckv_attend_ncache(const arckv_ncache *c, int32_t G, int32_t F, float scale, const void *Q,
+                                 const float *beta, const int32_t *length, const void *K_f, const void *V_f,
+                                 const int32_t *length_f, float *out, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------ rotary positions
+ * Turn rows of queries and keys by their positions.  With h = d_rot / 2, pair i < h of a row
+ * is its channels (i, i + h) (ARCKV_ROTARY_HALVES) or (2 i, 2 i + 1)
+ * (ARCKV_ROTARY_NEIGHBOURS), and for a token at position p, a = p * freq[i]:
+ *   (u, v) -> factor (u cos a - v sin a, u sin a + v cos a);
+ * channels from d_rot on are copied.  With transpose the turn is by -a: the transposed
+ * of that map, which takes the gradient of y to that of x (and, with factor 1, undoes it).
+ * Turning by a difference of positions moves keys that have been turned already.
+ * The angle is formed in float64 and reduced to one turn there, so that far positions
+ * keep their precision; its sine and cosine and the products are float32, and a
+ * bfloat16 result is rounded once. */
+typedef enum { ARCKV_ROTARY_HALVES = 0, ARCKV_ROTARY_NEIGHBOURS = 1 } arckv_rotary_layout;
+
+typedef struct {
+  int32_t N;          /* tokens, 1..2^26 */
+  int32_t d;          /* head dimension; must be 128 */
+  int32_t d_rot;      /* leading channels that are turned, even, 2..128 */
+  int32_t layout;     /* arckv_rotary_layout */
+  int32_t dtype;      /* arckv_dtype of x and y */
+  int32_t transpose;  /* 0 or 1 */
+  float factor;       /* finite; multiplies the turned channels */
+} arckv_rotary_params;
+
+/* Rows of one tensor: element (n, h, c) at x[n * x_token + h * x_head + c].  Strides in
+ * elements, >= 0, multiples of 16 bytes; x may repeat rows (stride 0), those of y must
+ * not overlap: its larger stride covers all that its smaller one spans.  y may be x with
+ * the same strides; it must share no row with x otherwise. */
+typedef struct {
+  int32_t heads;      /* 1..2^20 */
+  const void *x;
+  int64_t x_token, x_head;
+  void *y;
+  int64_t y_token, y_head;
+} arckv_rotary_rows;
+
+/*   positions [N] int32 device array, any sign, or NULL: token n is at position n;
+ *   freq      [d_rot / 2] float64 device array, radians per position;
+ *   a, b      rows that share the positions (a layer's queries and keys); b may be NULL.
+ * Tensors 16-byte aligned.  No workspace, no synchronisation. */
+arckv_status arckv_rotary(const arckv_rotary_params *p, const int32_t *positions, const double *freq,
+                          const arckv_rotary_rows *a, const arckv_rotary_rows *b, hipStream_t stream);
+
+/* Frequencies of the pairs (host only, no GPU work), with f_i = base^(-2 i / d_rot) and the
+ * context stretched to s = stretch times the `length` positions of training:
+ *   ARCKV_STRETCH_NONE    f_i
+ *   ARCKV_STRETCH_LINEAR  f_i / s (position interpolation)
+ *   ARCKV_STRETCH_BASE    f_i of the base  base * s^(d_rot / (d_rot - 2))  (d_rot > 2)
+ *   ARCKV_STRETCH_TURNS   g_i f_i + (1 - g_i) f_i / s by the turns r_i = length f_i / (2 pi) that a pair makes in
+ *                         training, g_i = clip_[0,1]((r_i - few) / (many - few))
+ *   ARCKV_STRETCH_INDEX   the same with g_i falling along i instead, from 1 at floor(c(many)) to 0 at ceil(c(few)),
+ *                         c(r) = d_rot log(length / (2 pi r)) / (2 log base), both clipped to [0, d_rot - 1]
+ *                         (their difference taken as 0.001 where they meet)
+ * freq: host array [d_rot / 2] output.  Needs a finite base > 1, and where they are used stretch >= 1,
+ * length > 0 and 0 < few < many, all finite. */
+typedef enum {
+  ARCKV_STRETCH_NONE = 0, ARCKV_STRETCH_LINEAR = 1, ARCKV_STRETCH_BASE = 2, ARCKV_STRETCH_TURNS = 3,
+  ARCKV_STRETCH_INDEX = 4
+} arckv_stretch;
+
+arckv_status arckv_rotary_frequencies(int32_t d_rot, double base, int32_t mode, double stretch, double length,
+                                      double few, double many, double *freq);
+
 /* Human-readable name of a status code (static string). */
 const char *arckv_status_string(arckv_status s);
 

@@ -21,6 +21,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
 E4M3, INT8 = 0, 1
 QBLOCK = 64          # tokens of an 8-bit cache that share a scale
+NGROUP = 32          # channels of a 4-bit cache's row that share a scale
 
 # Every entry point declared in include/arckv.h.
 ENTRY_POINTS = (
@@ -30,7 +31,8 @@ ENTRY_POINTS = (
     "arckv_attend_workspace_size", "arckv_attend", "arckv_budgets", "arckv_select_count", "arckv_select_ex",
     "arckv_dsa_workspace_size", "arckv_score_dsa", "arckv_compact_scored", "arckv_assign_stats",
     "arckv_attend_noalloc", "arckv_qcache_write", "arckv_qcache_read", "arckv_select_blocks",
-    "arckv_attend_qcache_workspace_size", "arckv_attend_qcache",
+    "arckv_attend_qcache_workspace_size", "arckv_attend_qcache", "arckv_ncache_write", "arckv_ncache_read",
+    "arckv_attend_ncache_workspace_size", "arckv_attend_ncache", "arckv_rotary", "arckv_rotary_frequencies",
 )
 
 
@@ -71,6 +73,22 @@ class QCacheStruct(ctypes.Structure):
     _fields_ = [("P", ctypes.c_int32), ("rows", ctypes.c_int32), ("d", ctypes.c_int32), ("format", ctypes.c_int32),
                 ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p),
                 ("V_scale", ctypes.c_void_p), ("K_bounds", ctypes.c_void_p)]
+
+
+class NCacheStruct(ctypes.Structure):
+    _fields_ = [("P", ctypes.c_int32), ("rows", ctypes.c_int32), ("d", ctypes.c_int32), ("K", ctypes.c_void_p),
+                ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p)]
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("d", ctypes.c_int32), ("d_rot", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("transpose", ctypes.c_int32), ("factor", ctypes.c_float)]
+
+
+class RotaryRows(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("x", ctypes.c_void_p), ("x_token", ctypes.c_int64),
+                ("x_head", ctypes.c_int64), ("y", ctypes.c_void_p), ("y_token", ctypes.c_int64),
+                ("y_head", ctypes.c_int64)]
 
 
 _LIB = None
@@ -118,6 +136,14 @@ def lib():
         L.arckv_select_blocks.argtypes = [QC, i32, ctypes.c_float, vp, vp, vp, i32, vp, vp, vp]
         L.arckv_attend_qcache_workspace_size.argtypes = [i32, i32, i32, i32, i32, P(sz)]
         L.arckv_attend_qcache.argtypes = [QC, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        NC = P(NCacheStruct)
+        L.arckv_ncache_write.argtypes = [NC, i32, i32, vp, vp, vp, vp, vp]
+        L.arckv_ncache_read.argtypes = [NC, i32, i32, i32, vp, vp, vp, vp]
+        L.arckv_attend_ncache_workspace_size.argtypes = [i32, i32, i32, i32, P(sz)]
+        L.arckv_attend_ncache.argtypes = [NC, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        f64 = ctypes.c_double
+        L.arckv_rotary.argtypes = [P(RotaryParams), vp, vp, P(RotaryRows), P(RotaryRows), vp]
+        L.arckv_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, P(f64)]
         L.arckv_assign_stats.argtypes = [P(Problem), i32, vp, sz, vp, vp]
         for name in ENTRY_POINTS:
             getattr(L, name).restype = ctypes.c_int if name != "arckv_status_string" else ctypes.c_char_p
@@ -605,6 +631,160 @@ def attend_qcache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f
                                      _qptr(length_f, row, torch.int32, dev, "length_f"), optr, wptr, nbytes,
                                      torch._C._cuda_getCurrentRawStream(dev)), "arckv_attend_qcache")
     return out
+
+
+class NCache(NamedTuple):
+    """The arrays of a 4-bit cache (arckv_ncache).  The functions below take any tuple of these four."""
+    K: torch.Tensor                     # codes [P][rows][64], uint8, two to a byte
+    V: torch.Tensor
+    K_scale: torch.Tensor               # [P][rows][4] uint8, exponent + 127 for every 32 channels
+    V_scale: torch.Tensor
+
+
+def ncache(P: int, rows: int, device="cuda") -> NCache:
+    """A 4-bit cache for P pairs of up to `rows` rows, nothing written yet (the arrays are uninitialised)."""
+    new = lambda width: torch.empty(P, rows, width, dtype=torch.uint8, device=device)
+    return NCache(new(64), new(64), new(128 // NGROUP), new(128 // NGROUP))
+
+
+def _ncache(c) -> tuple:
+    """(struct, P, rows, current device) of a cache tuple."""
+    K, V, Ks, Vs = c
+    dev = torch.cuda.current_device()
+    P, rows, width = K.shape
+    codes, scales, u8 = (P, rows, 64), (P, rows, 4), torch.uint8
+    return NCacheStruct(P, rows, 128, _qptr(K, codes, u8, dev, "K"), _qptr(V, codes, u8, dev, "V"),
+                        _qptr(Ks, scales, u8, dev, "K_scale"), _qptr(Vs, scales, u8, dev, "V_scale")), P, rows, dev
+
+
+def ncache_write(cache, K, V, start=None, count=None) -> None:
+    """arckv_ncache_write: rows K, V [P][n][128] (f32 or bf16) into the cache from row start[p] on, the first count[p]
+    of them (int32 [P] on the GPU; None: from row 0, all n)."""
+    st, P, rows, dev = _ncache(cache)
+    n, dtype = K.shape[1], K.dtype
+    shape, row, i32 = (P, n, 128), (P,), torch.int32
+    _check(lib().arckv_ncache_write(ctypes.byref(st), n, _dtype_code(dtype), _qptr(K, shape, dtype, dev, "K"),
+                                    _qptr(V, shape, dtype, dev, "V"), _qptr(start, row, i32, dev, "start"),
+                                    _qptr(count, row, i32, dev, "count"), torch._C._cuda_getCurrentRawStream(dev)),
+           "arckv_ncache_write")
+
+
+def ncache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bfloat16, length=None):
+    """arckv_ncache_read: rows first .. first + n - 1 as (K, V) [P][n][128] of dtype (f32 or bf16); zeros from row
+    length[p] (int32 [P]) on."""
+    first, n = _int32(first, "first"), n if n is None else _int32(n, "n")
+    st, P, rows, dev = _ncache(cache)
+    n = rows - first if n is None else n
+    code = _dtype_code(dtype)
+    K, V = torch.empty(2, P, min(max(n, 0), rows), 128, dtype=dtype, device=cache[0].device)
+    _check(lib().arckv_ncache_read(ctypes.byref(st), first, n, code, _qptr(length, (P,), torch.int32, dev, "length"),
+                                   K.data_ptr(), V.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
+           "arckv_ncache_read")
+    return K, V
+
+
+def attend_ncache_workspace_size(P: int, rows: int, G: int, F: int = 0) -> int:
+    out = ctypes.c_size_t()
+    args = [_int32(x, what) for x, what in ((P, "P"), (rows, "rows"), (G, "G"), (F, "F"))]
+    _check(lib().arckv_attend_ncache_workspace_size(*args, ctypes.byref(out)), "arckv_attend_ncache_workspace_size")
+    return out.value
+
+
+def attend_ncache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f=None, scale=None, out=None,
+                  ws=None) -> torch.Tensor:
+    """arckv_attend_ncache: decode attention of Q [P][G][128] bf16 over the cache's rows below length (int32 [P]) with
+    bias beta [P][rows] f32, and over the rows of K_f, V_f [P][F][128] bf16 below length_f.  out [P][G][128] f32 and ws
+    (uint8, attend_ncache_workspace_size bytes, 256-byte aligned) may be given; a workspace must not be shared by calls
+    that may overlap in time."""
+    st, P, rows, dev = _ncache(cache)
+    G = Q.shape[1]
+    F = K_f.shape[1] if K_f is not None else 0
+    row, tail, whole, i32, bf16 = (P,), (P, F, 128), (P, G, 128), torch.int32, torch.bfloat16
+    qptr = _qptr(Q, whole, bf16, dev, "Q")
+    if out is None:
+        out = torch.empty(whole, dtype=torch.float32, device=Q.device)
+        optr = out.data_ptr()
+    else:
+        optr = _qptr(out, whole, torch.float32, dev, "out")
+    if ws is None:
+        nbytes = ctypes.c_size_t()
+        _check(lib().arckv_attend_ncache_workspace_size(P, rows, G, F, ctypes.byref(nbytes)),
+               "arckv_attend_ncache_workspace_size")
+        nbytes = nbytes.value
+        # torch's device allocations are 512-byte aligned
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
+        wptr = ws.data_ptr() if nbytes else None
+    else:
+        nbytes = ws.numel()
+        wptr = _qptr(ws, ws.shape, torch.uint8, dev, "ws")
+    _check(lib().arckv_attend_ncache(ctypes.byref(st), G, F, float(scale) if scale else 0.0, qptr,
+                                     _qptr(beta, (P, rows), torch.float32, dev, "beta"),
+                                     _qptr(length, row, i32, dev, "length"), _qptr(K_f, tail, bf16, dev, "K_f"),
+                                     _qptr(V_f, tail, bf16, dev, "V_f"), _qptr(length_f, row, i32, dev, "length_f"), optr,
+                                     wptr, nbytes, torch._C._cuda_getCurrentRawStream(dev)), "arckv_attend_ncache")
+    return out
+
+
+STRETCHES = ("none", "linear", "base", "turns", "index")
+
+
+def rotary_frequencies(d_rot: int = 128, base: float = 10000.0, mode: str = "none", stretch: float = 1.0,
+                       length: float = 0.0, few: float = 1.0, many: float = 32.0, device="cuda") -> torch.Tensor:
+    """arckv_rotary_frequencies: radians per position of the d_rot / 2 pairs, float64 on the device, for a context
+    stretched by one of STRETCHES."""
+    if mode not in STRETCHES:
+        raise ValueError(f"mode: {mode!r} is none of {STRETCHES}")
+    d_rot = _int32(d_rot, "d_rot")
+    out = (ctypes.c_double * max(1, min(d_rot, 128) // 2))()
+    _check(lib().arckv_rotary_frequencies(d_rot, float(base), STRETCHES.index(mode), float(stretch), float(length),
+                                          float(few), float(many), out), "arckv_rotary_frequencies")
+    return torch.tensor(list(out), dtype=torch.float64, device=device)
+
+
+def _rotary_rows(x, y, N: int, dtype, dev: int, what: str) -> RotaryRows:
+    """x [N][heads][128] into y, both with any strides of tokens and heads."""
+    shape = x.shape
+    for t, name in ((x, what), (y, what + "'s output")):
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+        if len(shape) != 3 or shape[0] != N or shape[2] != 128 or t.shape != shape:
+            raise ValueError(f"{name}: expected shape ({N}, heads, 128), got {tuple(t.shape)}")
+        if t.stride(2) != 1:
+            raise ValueError(f"{name}: a row's channels must be contiguous")
+    if x.get_device() != dev or y.get_device() != dev:
+        raise ValueError(f"{what}: tensors must live on the current GPU")
+    heads = shape[1]
+    xt, xh, _ = x.stride()
+    yt, yh, _ = y.stride()
+    if N == 1:              # the stride of an axis of one says nothing
+        xt = yt = 0
+    if heads == 1:
+        xh = yh = 0
+    return RotaryRows(heads, x.data_ptr(), xt, xh, y.data_ptr(), yt, yh)
+
+
+def rotary(x, freq, positions=None, other=None, interleaved: bool = False, transpose: bool = False, factor: float = 1.0,
+           out=None, out_other=None):
+    """arckv_rotary: rows x [N][heads][128] (f32 or bf16) turned by positions (int32 [N] on the GPU; None: 0 .. N - 1)
+    times freq (float64 [d_rot / 2], rotary_frequencies), pairs of halves or, interleaved, of neighbours; with
+    transpose, its gradient's way back.  `other` are rows of the same tokens (a layer's keys beside its queries), turned
+    by the same call.  Strides of tokens and heads are free; out and out_other may be given (the inputs themselves, or
+    tensors that share no row with them).  Returns out, or (out, out_other)."""
+    dev, dtype = torch.cuda.current_device(), x.dtype
+    N, pairs = x.shape[0], freq.shape[0]
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    p = RotaryParams(N, 128, 2 * pairs, 1 if interleaved else 0, _dtype_code(dtype), 1 if transpose else 0, factor)
+    a = _rotary_rows(x, out, N, dtype, dev, "x")
+    b = None
+    if other is not None:
+        if out_other is None:
+            out_other = torch.empty(other.shape, dtype=dtype, device=other.device)
+        b = ctypes.byref(_rotary_rows(other, out_other, N, dtype, dev, "other"))
+    _check(lib().arckv_rotary(ctypes.byref(p), _qptr(positions, (N,), torch.int32, dev, "positions"),
+                              _qptr(freq, (pairs,), torch.float64, dev, "freq"), ctypes.byref(a), b,
+                              torch._C._cuda_getCurrentRawStream(dev)), "arckv_rotary")
+    return out if other is None else (out, out_other)
 
 
 def set_timing(enable: bool):

@@ -1,5 +1,6 @@
 // Host side of the ARC-KV library: argument validation (before any HIP call),
 // workspace planning, and stage sequencing on the caller's stream.
+#include <initializer_list>
 #include <math.h>
 #include <mutex>
 #include <stdint.h>
@@ -11,7 +12,9 @@
 #include "arckv.h"
 #include "assign.hpp"
 #include "fit.hpp"
+#include "ncache.hpp"
 #include "qcache.hpp"
+#include "rotary.hpp"
 
 namespace arckv {
 typedef uint16_t bf16_t_;   // bfloat16 storage, opaque on the host
@@ -134,19 +137,30 @@ int attendq_chunks(int P, int nsel, int F, int *iters);
 hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const int32_t *blocks, int nsel, const void *Kf, const void *Vf,
                           const int32_t *length_f, float *part_o, float *part_ml, float *out, hipStream_t s);
+hipError_t launch_ncache_write(int dtype, const NCache &c, int n, const void *K, const void *V, const int32_t *start,
+                               const int32_t *count, hipStream_t s);
+hipError_t launch_ncache_read(int dtype, const NCache &c, int first, int n, const int32_t *length, void *K, void *V,
+                              hipStream_t s);
+int attendn_chunks(int P, int rows, int F);
+hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void *Q, const float *beta,
+                          const int32_t *length, const void *Kf, const void *Vf, const int32_t *length_f, float *part_o,
+                          float *part_ml, float *out, hipStream_t s);
+hipError_t launch_rotary(int dtype, const Rotary &a, hipStream_t s);
 
 // ------------------------------------------------------------------ timing
 enum Stage {
   ST_SCORE, ST_SELECT, ST_ROWSTATS, ST_ZMAX, ST_PROFILES, ST_ANCHOR_PROF, ST_ASSIGN, ST_FINALIZE, ST_MERGE,
   ST_PHIC, ST_GRAM_G, ST_CHOL_G, ST_SOLVE_W, ST_PHAT, ST_GRAM_A, ST_RHS, ST_CHOL_A, ST_SOLVE_V, ST_ATTEND,
   ST_DSA_PROJ, ST_DSA_VALUE, ST_DSA_INDEX, ST_ASSIGN_REFINE, ST_ASSIGN_EXACT,
-  ST_QCACHE_WRITE, ST_QCACHE_READ, ST_SELECT_BLOCKS, ST_ATTEND_QCACHE, ST_COUNT
+  ST_QCACHE_WRITE, ST_QCACHE_READ, ST_SELECT_BLOCKS, ST_ATTEND_QCACHE,
+  ST_NCACHE_WRITE, ST_NCACHE_READ, ST_ATTEND_NCACHE, ST_ROTARY, ST_COUNT
 };
 static const char *kStageNames[ST_COUNT] = {
     "score", "select", "rowstats", "zmax", "profiles", "anchor_profiles", "assign_gemm", "assign_finalize",
     "merge", "phic", "gram_G", "chol_G", "solve_beta", "phat", "gram_A", "rhs_B", "chol_A", "solve_values",
     "attend", "dsa_proj", "dsa_value_head", "dsa_index", "assign_refine", "assign_exact",
-    "qcache_write", "qcache_read", "select_blocks", "attend_qcache"};
+    "qcache_write", "qcache_read", "select_blocks", "attend_qcache",
+    "ncache_write", "ncache_read", "attend_ncache", "rotary"};
 
 struct TimingState {
   std::mutex mu;
@@ -1097,6 +1111,167 @@ arckv_status arckv_attend_qcache(const arckv_qcache *c, int32_t G, int32_t nsel,
   STAGE(ST_ATTEND_QCACHE,
         launch_attendq(c->format, make_qcache(c), G, F, s, Q, beta, length, blocks, nsel, F > 0 ? K_f : nullptr,
                        F > 0 ? V_f : nullptr, length_f, (float *)ws, need ? (float *)((char *)ws + ml) : nullptr, out, stream));
+  return ARCKV_OK;
+}
+
+// ---------------------------------------------------------------- 4-bit cache
+static arckv_status check_ncache(const arckv_ncache *c) {
+  if (!c || c->P < 1 || c->rows < 1) return ARCKV_ERR_INVALID_ARG;
+  if (c->d != kHeadDimH || c->rows > kQRowsMax || c->P > kQPairsMax) return ARCKV_ERR_UNSUPPORTED;
+  if (!c->K || !c->V || !c->K_scale || !c->V_scale) return ARCKV_ERR_INVALID_ARG;
+  if (!aligned(c->K, 16) || !aligned(c->V, 16) || !aligned(c->K_scale, 4) || !aligned(c->V_scale, 4))
+    return ARCKV_ERR_INVALID_ARG;
+  return ARCKV_OK;
+}
+
+static NCache make_ncache(const arckv_ncache *c) {
+  return NCache{(uint8_t *)c->K, (uint8_t *)c->V, (uint32_t *)c->K_scale, (uint32_t *)c->V_scale, c->P, c->rows};
+}
+
+arckv_status arckv_ncache_write(const arckv_ncache *c, int32_t n, int32_t dtype, const void *K, const void *V,
+                                const int32_t *start, const int32_t *count, hipStream_t stream) {
+  CHECK(check_ncache(c));
+  if (n < 1 || n > c->rows || !K || !V || !aligned(K, 16) || !aligned(V, 16) || !aligned(start, 4) || !aligned(count, 4))
+    return ARCKV_ERR_INVALID_ARG;
+  if (dtype != ARCKV_F32 && dtype != ARCKV_BF16) return ARCKV_ERR_UNSUPPORTED;
+  STAGE(ST_NCACHE_WRITE, launch_ncache_write(dtype, make_ncache(c), n, K, V, start, count, stream));
+  return ARCKV_OK;
+}
+
+arckv_status arckv_ncache_read(const arckv_ncache *c, int32_t first, int32_t n, int32_t dtype, const int32_t *length,
+                               void *K, void *V, hipStream_t stream) {
+  CHECK(check_ncache(c));
+  if (first < 0 || n < 1 || n > c->rows || first > c->rows - n) return ARCKV_ERR_INVALID_ARG;
+  if (!K || !V || !aligned(K, 16) || !aligned(V, 16) || !aligned(length, 4)) return ARCKV_ERR_INVALID_ARG;
+  if (dtype != ARCKV_F32 && dtype != ARCKV_BF16) return ARCKV_ERR_UNSUPPORTED;
+  STAGE(ST_NCACHE_READ, launch_ncache_read(dtype, make_ncache(c), first, n, length, K, V, stream));
+  return ARCKV_OK;
+}
+
+static arckv_status check_attend_ncache(int32_t P, int32_t rows, int32_t G, int32_t F) {
+  if (P < 1 || rows < 1 || G < 1 || F < 0) return ARCKV_ERR_INVALID_ARG;
+  if (G > 16 || P > kQPairsMax || rows > kQRowsMax || F > kQRowsMax) return ARCKV_ERR_UNSUPPORTED;
+  return ARCKV_OK;
+}
+
+static size_t attend_ncache_ws_bytes(int32_t P, int32_t rows, int32_t G, int32_t F, size_t *ml) {
+  const size_t nch = (size_t)attendn_chunks(P, rows, F);
+  *ml = (size_t)rup((int64_t)((size_t)P * nch * G * kHeadDimH * 4), 256);
+  return nch == 1 ? 0 : *ml + (size_t)rup((int64_t)((size_t)P * nch * G * 2 * 4), 256);
+}
+
+arckv_status arckv_attend_ncache_workspace_size(int32_t P, int32_t rows, int32_t G, int32_t F, size_t *bytes) {
+  CHECK(check_attend_ncache(P, rows, G, F));
+  if (!bytes) return ARCKV_ERR_INVALID_ARG;
+  size_t ml;
+  *bytes = attend_ncache_ws_bytes(P, rows, G, F, &ml);
+  return ARCKV_OK;
+}
+
+arckv_status arckv_attend_ncache(const arckv_ncache *c, int32_t G, int32_t F, float scale, const void *Q,
+                                 const float *beta, const int32_t *length, const void *K_f, const void *V_f,
+                                 const int32_t *length_f, float *out, void *ws, size_t ws_bytes, hipStream_t stream) {
+  CHECK(check_ncache(c));
+  CHECK(check_attend_ncache(c->P, c->rows, G, F));
+  if (!Q || !out || (F > 0 && (!K_f || !V_f))) return ARCKV_ERR_INVALID_ARG;
+  if (!isfinite(scale) || !aligned(Q, 16) || !aligned(beta, 4) || !aligned(length, 4) || !aligned(K_f, 16) ||
+      !aligned(V_f, 16) || !aligned(length_f, 4) || !aligned(out, 16))
+    return ARCKV_ERR_INVALID_ARG;
+  size_t ml;
+  const size_t need = attend_ncache_ws_bytes(c->P, c->rows, G, F, &ml);
+  if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return ARCKV_ERR_WORKSPACE;
+  const float s = scale > 0.0f ? scale : 1.0f / sqrtf((float)kHeadDimH);
+  STAGE(ST_ATTEND_NCACHE,
+        launch_attendn(make_ncache(c), G, F, s, Q, beta, length, F > 0 ? K_f : nullptr, F > 0 ? V_f : nullptr, length_f,
+                       (float *)ws, need ? (float *)((char *)ws + ml) : nullptr, out, stream));
+  return ARCKV_OK;
+}
+
+// ---------------------------------------------------------------- rotary positions
+constexpr int32_t kRotaryTokensMax = 1 << 26;
+constexpr int32_t kRotaryHeadsMax = 1 << 20;
+constexpr int64_t kRotaryStrideMax = (int64_t)1 << 34;   // elements; offsets stay below 2^60
+
+static arckv_status check_rotary_rows(const arckv_rotary_rows *r, int32_t N, int width) {
+  if (r->heads < 1 || !r->x || !r->y || !aligned(r->x, 16) || !aligned(r->y, 16)) return ARCKV_ERR_INVALID_ARG;
+  if (r->heads > kRotaryHeadsMax) return ARCKV_ERR_UNSUPPORTED;
+  for (const int64_t s : {r->x_token, r->x_head, r->y_token, r->y_head}) {
+    if (s < 0 || s % (16 / width) != 0) return ARCKV_ERR_INVALID_ARG;
+    if (s > kRotaryStrideMax) return ARCKV_ERR_UNSUPPORTED;
+  }
+  // rows of y apart from each other: along the axis with the smaller stride, and along the other beyond all of those
+  const bool by_token = N > 1, by_head = r->heads > 1;
+  if ((by_token && r->y_token < kHeadDimH) || (by_head && r->y_head < kHeadDimH)) return ARCKV_ERR_INVALID_ARG;
+  if (by_token && by_head) {
+    const bool heads_inside = r->y_head <= r->y_token;
+    const int64_t inner = heads_inside ? r->y_head : r->y_token, outer = heads_inside ? r->y_token : r->y_head;
+    if (outer < inner * ((heads_inside ? r->heads : N) - 1) + kHeadDimH) return ARCKV_ERR_INVALID_ARG;
+  }
+  if (r->x == r->y && ((by_token && r->x_token != r->y_token) || (by_head && r->x_head != r->y_head)))
+    return ARCKV_ERR_INVALID_ARG;
+  return ARCKV_OK;
+}
+
+arckv_status arckv_rotary(const arckv_rotary_params *p, const int32_t *positions, const double *freq,
+                          const arckv_rotary_rows *a, const arckv_rotary_rows *b, hipStream_t stream) {
+  if (!p || !a || !freq || p->N < 1) return ARCKV_ERR_INVALID_ARG;
+  if (p->d != kHeadDimH || p->N > kRotaryTokensMax) return ARCKV_ERR_UNSUPPORTED;
+  if (p->d_rot < 2 || p->d_rot > p->d || p->d_rot % 2 != 0 || !isfinite(p->factor)) return ARCKV_ERR_INVALID_ARG;
+  if (p->layout != ARCKV_ROTARY_HALVES && p->layout != ARCKV_ROTARY_NEIGHBOURS) return ARCKV_ERR_UNSUPPORTED;
+  if (p->dtype != ARCKV_F32 && p->dtype != ARCKV_BF16) return ARCKV_ERR_UNSUPPORTED;
+  if ((p->transpose != 0 && p->transpose != 1) || !aligned(positions, 4) || !aligned(freq, 8)) return ARCKV_ERR_INVALID_ARG;
+  const int width = p->dtype == ARCKV_F32 ? 4 : 2;
+  CHECK(check_rotary_rows(a, p->N, width));
+  if (b) CHECK(check_rotary_rows(b, p->N, width));
+  Rotary r{};
+  const arckv_rotary_rows *rows[2] = {a, b};
+  for (int i = 0; i < 2; ++i)
+    if (rows[i]) {
+      r.r[i] = RotaryRows{rows[i]->x, rows[i]->y, rows[i]->x_token, rows[i]->x_head, rows[i]->y_token, rows[i]->y_head};
+      r.heads[i] = rows[i]->heads;
+    }
+  r.N = p->N;
+  r.half = p->d_rot / 2;
+  r.neighbours = p->layout == ARCKV_ROTARY_NEIGHBOURS;
+  r.sign = p->transpose ? -1.0f : 1.0f;
+  r.factor = p->factor;
+  r.positions = positions;
+  r.freq = freq;
+  STAGE(ST_ROTARY, launch_rotary(p->dtype, r, stream));
+  return ARCKV_OK;
+}
+
+arckv_status arckv_rotary_frequencies(int32_t d_rot, double base, int32_t mode, double stretch, double length,
+                                      double few, double many, double *freq) {
+  constexpr double kTurn = 6.283185307179586477;
+  if (d_rot < 2 || d_rot > kHeadDimH || d_rot % 2 != 0 || !freq || !isfinite(base) || !(base > 1.0))
+    return ARCKV_ERR_INVALID_ARG;
+  if (mode < ARCKV_STRETCH_NONE || mode > ARCKV_STRETCH_INDEX) return ARCKV_ERR_UNSUPPORTED;
+  if (mode != ARCKV_STRETCH_NONE && (!isfinite(stretch) || !(stretch >= 1.0))) return ARCKV_ERR_INVALID_ARG;
+  const bool ramp = mode == ARCKV_STRETCH_TURNS || mode == ARCKV_STRETCH_INDEX;
+  if (ramp && (!isfinite(length) || !(length > 0.0) || !isfinite(many) || !(few > 0.0) || !(many > few)))
+    return ARCKV_ERR_INVALID_ARG;
+  if (mode == ARCKV_STRETCH_BASE) {
+    if (d_rot == 2) return ARCKV_ERR_INVALID_ARG;
+    base *= pow(stretch, (double)d_rot / (d_rot - 2));
+    if (!isfinite(base)) return ARCKV_ERR_INVALID_ARG;
+  }
+  auto clip = [](double x, double most) { return x < 0.0 ? 0.0 : x > most ? most : x; };
+  double from = 0.0, to = 0.0;   // INDEX: the ramp's ends
+  if (mode == ARCKV_STRETCH_INDEX) {
+    auto pair_of = [&](double turns) { return d_rot * log(length / (kTurn * turns)) / (2.0 * log(base)); };
+    from = clip(floor(pair_of(many)), d_rot - 1);
+    to = clip(ceil(pair_of(few)), d_rot - 1);
+    if (to == from) to += 0.001;
+  }
+  for (int i = 0; i < d_rot / 2; ++i) {
+    const double f = pow(base, -2.0 * i / d_rot);
+    double keep = 1.0;
+    if (mode == ARCKV_STRETCH_LINEAR) keep = 0.0;
+    if (mode == ARCKV_STRETCH_TURNS) keep = clip((length * f / kTurn - few) / (many - few), 1.0);
+    if (mode == ARCKV_STRETCH_INDEX) keep = 1.0 - clip((i - from) / (to - from), 1.0);
+    freq[i] = mode == ARCKV_STRETCH_NONE || mode == ARCKV_STRETCH_BASE ? f : keep * f + (1.0 - keep) * f / stretch;
+  }
   return ARCKV_OK;
 }
 

@@ -1,0 +1,235 @@
+"""Rotary positions on the GPU against the float64 oracle.
+
+Tolerance of an element, u = 2^-24: the turns' fraction is rounded to float32 (at most 2^-26 of a turn, 2 pi 2^-26 < 1.6 u rad),
+sine and cosine are within 4 ulp (4 u), the factor rounds once (u), products and sum three times: with A the angle's
+float64 error (three roundings of 2^-53 of up to `turns` turns),
+  |dy| <= f (|x_u| + |x_v|) (1.6 + 4 + 1 + 3) u (1 + tiny) + A f (|x_u| + |x_v|),
+and half a step of the type at the end.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import rotary as orot
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def A():
+    from paper_2609_36835_amd import arckv
+    return arckv
+
+
+def np64(x):
+    return x.double().cpu().numpy()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def rows(g, *shape, dtype=torch.bfloat16):
+    return torch.from_numpy(g.standard_normal(shape).astype(np.float32)).cuda().to(dtype)
+
+
+def check(got, x, pos, freq, interleaved=False, transpose=False, factor=1.0):
+    x, h, f = np64(x), len(freq), np64(freq)
+    want = orot.rotary(x, pos, f, interleaved, transpose, factor)
+    mag = np.zeros_like(x)
+    u, v = (slice(0, 2 * h, 2), slice(1, 2 * h, 2)) if interleaved else (slice(0, h), slice(h, 2 * h))
+    mag[..., u] = mag[..., v] = (np.abs(x[..., u]) + np.abs(x[..., v])) * abs(factor)
+    turns = np.abs(np.asarray(pos, np.float64)).max() * np.abs(f).max() / (2 * math.pi)
+    tol = mag * (9.7 * U + 2 * math.pi * 3 * 2.0 ** -53 * turns) + np.abs(want) * torch.finfo(got.dtype).eps / 2
+    tol = tol + (mag > 0) * 1e-37
+    d = np.abs(np64(got) - want)
+    assert (d <= tol).all(), (np.argwhere(d > tol)[:4], (d - tol).max())
+    assert np.array_equal(np64(got)[..., 2 * h:], x[..., 2 * h:])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d_rot", [2, 6, 16, 32, 34, 64, 96, 112, 126, 128])
+def test_turns(dtype, interleaved, d_rot):
+    g = np.random.default_rng(d_rot)
+    freq = A().rotary_frequencies(d_rot, 500000.0)
+    for N, H, K in [(1, 1, 0), (1, 32, 8), (2, 3, 1), (7, 1, 1), (33, 5, 2), (300, 2, 0), (65, 16, 16)]:
+        print(f"turns {dtype} interleaved={interleaved} d_rot={d_rot} N={N} H={H} K={K}", flush=True)
+        pos = g.integers(0, 131072, N)
+        x = rows(g, N, H, 128, dtype=dtype)
+        if K:
+            k = rows(g, N, K, 128, dtype=dtype)
+            y, z = A().rotary(x, freq, i32(pos), k, interleaved=interleaved)
+            check(z, k, pos, freq, interleaved)
+        else:
+            y = A().rotary(x, freq, i32(pos), interleaved=interleaved)
+        check(y, x, pos, freq, interleaved)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d_rot", [64, 96, 30, 128])
+def test_strides(dtype, interleaved, d_rot):
+    """Queries and keys out of a fused projection into tensors [head][token], one head for all, and in place; what lies
+    between the rows stays."""
+    g = np.random.default_rng(1)
+    N, H, K = 37, 4, 2
+    freq, pos = A().rotary_frequencies(d_rot, 10000.0), g.integers(0, 5000, N)
+    qkv = rows(g, N, H + 2 * K, 128, dtype=dtype)
+    kept = qkv.clone()
+    q, k = qkv[:, :H], qkv[:, H:H + K]
+    qo, ko = torch.full((H, N, 128), 7.0, dtype=dtype, device="cuda"), torch.full((K, N + 3, 128), 7.0, dtype=dtype, device="cuda")
+    A().rotary(q, freq, i32(pos), k, interleaved=interleaved, out=qo.transpose(0, 1), out_other=ko[:, :N].transpose(0, 1))
+    assert torch.equal(qkv, kept) and (ko[:, N:] == 7).all()
+    check(qo.transpose(0, 1), q, pos, freq, interleaved)
+    check(ko[:, :N].transpose(0, 1), k, pos, freq, interleaved)
+    one = qkv[:, :1].expand(N, 5, 128)                   # five heads of the same row
+    check(A().rotary(one, freq, i32(pos), interleaved=interleaved), one, pos, freq, interleaved)
+    A().rotary(q, freq, i32(pos), k, interleaved=interleaved, out=q, out_other=k)
+    check(q, kept[:, :H], pos, freq, interleaved)
+    check(k, kept[:, H:H + K], pos, freq, interleaved)
+    assert torch.equal(qkv[:, H + K:], kept[:, H + K:])
+    with pytest.raises(A().ArckvError):
+        A().rotary(q, freq, i32(pos), out=torch.empty(1, H, 128, dtype=dtype, device="cuda").expand(N, H, 128))
+    odd = torch.empty(N * 132, dtype=dtype, device="cuda").as_strided((N, 1, 128), (129, 128, 1))
+    with pytest.raises(A().ArckvError):
+        A().rotary(q[:, :1], freq, i32(pos), out=odd)
+
+
+def test_far_and_negative_positions():
+    """Up to 31 bits, either sign, and none given; zero turns nothing."""
+    g = np.random.default_rng(2)
+    freq = A().rotary_frequencies(128, 10000.0)
+    pos = [0, 1, -1, 1 << 20, -(1 << 20), (1 << 24) + 1, 2 ** 31 - 1, -2 ** 31]
+    x = rows(g, 8, 3, 128, dtype=torch.float32)
+    y = A().rotary(x, freq, i32(pos))
+    check(y, x, pos, freq)
+    assert torch.equal(y[0], x[0])
+    check(A().rotary(x, freq), x, np.arange(8), freq)
+    b = A().rotary(x, freq, i32(pos), transpose=True)
+    check(b, x, pos, freq, transpose=True)
+
+
+@pytest.mark.parametrize("mode,factor", [("linear", 1.0), ("base", 1.0), ("turns", 0.1 * math.log(8.0) + 1.0), ("index", 1.5)])
+def test_stretched(mode, factor):
+    g = np.random.default_rng(3)
+    freq = A().rotary_frequencies(96, 10000.0, mode, 8.0, 4096.0, 1.0, 32.0)
+    pos = g.integers(0, 32768, 40)
+    x = rows(g, 40, 4, 128)
+    check(A().rotary(x, freq, i32(pos), factor=factor), x, pos, freq, factor=factor)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d_rot", [22, 64, 128])
+def test_gradient(interleaved, d_rot):
+    """transpose is the gradient: against autograd of the formula in float64, and against differences of the forward call
+    (which is linear, so a difference over any step is the derivative, up to the call's own roundings)."""
+    g = np.random.default_rng(4)
+    N, H, f = 6, 3, 1.25
+    freq, pos = A().rotary_frequencies(d_rot, 10000.0), g.integers(0, 3000, N)
+    x, gy = rows(g, N, H, 128, dtype=torch.float32), rows(g, N, H, 128, dtype=torch.float32)
+    gx = A().rotary(gy, freq, i32(pos), interleaved=interleaved, transpose=True, factor=f)
+    check(gx, gy, pos, freq, interleaved, True, f)
+    xa = x.double().cpu().requires_grad_()
+    h = d_rot // 2
+    a = torch.from_numpy(pos).double()[:, None, None] * freq.cpu()
+    u, v = (xa[..., 0:2 * h:2], xa[..., 1:2 * h:2]) if interleaved else (xa[..., :h], xa[..., h:2 * h])
+    yu, yv = f * (u * a.cos() - v * a.sin()), f * (u * a.sin() + v * a.cos())
+    head = torch.stack([yu, yv], -1).flatten(-2) if interleaved else torch.cat([yu, yv], -1)
+    torch.cat([head, xa[..., 2 * h:]], -1).backward(gy.double().cpu())
+    want = xa.grad.numpy()
+    gyn = np.abs(np64(gy))
+    assert (np.abs(np64(gx) - want) <= 12 * U * f * 2 * gyn.max()).all()
+    y0 = np64(A().rotary(x, freq, i32(pos), interleaved=interleaved, factor=f))
+    for n, hd, c in [(0, 0, 0), (1, 2, 1), (2, 1, h), (3, 0, 2 * h - 1), (4, 1, 127), (5, 2, 2 * h - 2)]:
+        xd = x.clone()
+        xd[n, hd, c] += 4.0
+        d = (np64(A().rotary(xd, freq, i32(pos), interleaved=interleaved, factor=f)) - y0) / 4
+        big = np.abs(np64(xd)).max() * 2 * f
+        assert abs((d * np64(gy)).sum() - np64(gx)[n, hd, c]) <= 2 * 12 * U * big * 2 * gyn.max(), (n, hd, c)
+    back = A().rotary(A().rotary(x, freq, i32(pos), interleaved=interleaved), freq, i32(pos), interleaved=interleaved, transpose=True)
+    assert (back - x).abs().max() <= 2 * 12 * U * 2 * x.abs().max()
+
+
+def test_moves_compact_keys():
+    """Keys that were turned at their old places, turned on by the difference, are the keys at the new places."""
+    g = np.random.default_rng(5)
+    P, t = 3, 50
+    freq = A().rotary_frequencies(128, 500000.0)
+    old, new = np.sort(g.integers(0, 30000, (P, t))), np.tile(np.arange(t), (P, 1))
+    raw = rows(g, P * t, 1, 128, dtype=torch.float32)
+    K = A().rotary(raw, freq, i32(old.reshape(-1)))
+    A().rotary(K, freq, i32((new - old).reshape(-1)), out=K)
+    want = orot.rotary(np64(raw), new.reshape(-1), np64(freq))
+    assert (np.abs(np64(K) - want) <= 2 * 12 * U * 2 * np64(raw).max()).all()
+
+
+def test_non_finite_values_stay_in_their_pair():
+    freq = A().rotary_frequencies(64, 10000.0)
+    x = torch.ones(3, 2, 128, device="cuda")
+    x[1, 0, 3] = math.nan
+    x[2, 1, 100] = math.inf
+    for inter, mate in ((False, 35), (True, 2)):
+        y = A().rotary(x, freq, i32([5, 6, 7]), interleaved=inter)
+        bad = (~y.isfinite()).nonzero().tolist()
+        assert bad == sorted([[1, 0, 3], [1, 0, mate], [2, 1, 100]])
+
+
+def test_many_tokens_and_heads():
+    """Grids beyond one extent, a stride that passes 32 bits, and the last rows of each."""
+    g = np.random.default_rng(6)
+    freq = A().rotary_frequencies(128, 10000.0)
+    N = (1 << 21) + 5
+    x = torch.zeros(N, 1, 128, dtype=torch.bfloat16, device="cuda")
+    tail = rows(g, 3, 1, 128)
+    x[-3:] = tail
+    x[:2] = tail[:2]
+    y = A().rotary(x, freq)
+    check(y[-3:], tail, np.arange(N - 3, N), freq)
+    check(y[:2], tail[:2], [0, 1], freq)
+    assert (y[2:-3] == 0).all()
+    del x, y
+    base = torch.zeros((1 << 32) + 4096, dtype=torch.uint8, device="cuda").view(torch.bfloat16)
+    far = base.as_strided((2, 2, 128), (1 << 31, 256, 1))
+    x = rows(g, 2, 2, 128)
+    far.copy_(x)
+    check(A().rotary(far, freq, i32([9, 10])), x, [9, 10], freq)
+    A().rotary(x, freq, i32([11, 12]), out=far)
+    check(far, x, [11, 12], freq)
+    h = rows(g, 2, 5000, 128)
+    check(A().rotary(h, freq, i32([3, 70000])), h, [3, 70000], freq)
+
+
+def test_streams_and_graphs():
+    """Two streams at once, and a captured call replayed on new inputs with eager work between."""
+    g = np.random.default_rng(7)
+    freq = A().rotary_frequencies(128, 500000.0)
+    q, k, pos = rows(g, 64, 8, 128), rows(g, 64, 2, 128), i32(list(range(64)))
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    call = lambda: A().rotary(q, freq, pos, k, out=qo, out_other=ko)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for r in range(4):
+        q.copy_(rows(g, 64, 8, 128))
+        k.copy_(rows(g, 64, 2, 128))
+        p = g.integers(0, 100000, 64)
+        pos.copy_(i32(p))
+        graph.replay()
+        check(qo, q, p, freq)
+        check(ko, k, p, freq)
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(other):
+            y = A().rotary(q, freq, pos, transpose=True)
+        z = A().rotary(k, freq, pos, transpose=True)
+        torch.cuda.synchronize()
+        check(y, q, p, freq, transpose=True)
+        check(z, k, p, freq, transpose=True)

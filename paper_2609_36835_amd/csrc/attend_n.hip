@@ -4,11 +4,41 @@
 // over the rows below the pair's lengths whose bias is not -inf; a pair with
 // none of them gets zeros.
 //
-// One workgroup per query row: a wave takes every fourth row, a lane two channels, with a running softmax; the waves
-// meet in LDS.
+// HBM-bound: 136 bytes per token.  Split-key in two kernels:
+//   k_attendn_partial  a workgroup takes a share of the pair's units (blocks of 64 rows, 32 rows of the tail), a wave a
+//                      unit at a time, with a running softmax.
+//   k_attend_combine   merges the partials of a pair; a call of one chunk per pair needs none.
+//
+// Logits.  Keys go to MFMA 16x16x128 as they are held, codes and scales, so that nothing is unpacked.  Its other operand
+// is 8-bit, and it aligns the products of neighbouring channels to the largest of them, 13 bits below which it cuts.  So a
+// query enters as four planes, q = sum_t p_t 2^(E - 5 t), with 2^E above the magnitudes of its 32 channels and each p_t the
+// nearest e4m3 number to what the planes before it left, in magnitude at most 2, in units of 2^-9: products with codes (units
+// of 0.5, at most 6) are whole numbers of 2^-10 and stay within the 13 bits, so every sum is exact up to its float32 rounding,
+// and what the four planes leave is below 2^(E - 25).  2^(E - 5 t) is the operand's scale.  The planes are columns beside the
+// queries (up to 4 queries fill 16 columns), or products of their own (more queries).
+//
+// Values become bf16, scale included, in registers (exact); probabilities enter (P V)^T as three bf16 terms that sum to
+// them exactly, as columns beside the queries again where there is room.  The columns of both products are the same queries,
+// so a query's sums sit with its running maximum.
+#include <type_traits>
+
+#include "attend_parts.hpp"
 #include "ncode.hpp"
 
 namespace arckv {
+
+namespace {
+constexpr int kAnBlock = 64;          // rows of a unit
+constexpr int kAnW = 4;               // waves per workgroup
+constexpr int kAnWide = 16;           // of one that takes a whole pair of a small call, one unit per wave
+constexpr int kAnSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
+constexpr int kAnStart = 6;           // cost of a workgroup beside its units, in units per wave
+constexpr int kAnPlanes = 4;
+// Bytes above which codes are read as streams that the caches do not keep.
+constexpr int64_t kAnKept = (int64_t)64 << 20;
+
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+}  // namespace
 
 struct AttendN {
   NCache c;
@@ -20,63 +50,389 @@ struct AttendN {
   const bf16 *Kf, *Vf;
   const int32_t *length_f;
   float *part_o, *part_ml, *out;
+  int nch;                    // chunks per pair
 };
 
-__global__ void __launch_bounds__(256) k_attendn(AttendN a) {
-  __shared__ float sM[4], sL[4], sO[4][kHeadDim];
-  const int q = blockIdx.x, p = blockIdx.z * gridDim.y + blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (p >= a.c.P) return;
-  const bf16 *Q = a.Q + ((int64_t)p * a.G + q) * kHeadDim + 2 * lane;
-  const float q0 = (float)Q[0], q1 = (float)Q[1];
-  const int len = clip_len(a.length, p, a.c.rows), len_f = clip_len(a.length_f, p, a.F);
-  float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  auto take = [&](float k0, float k1, float v0, float v1, float bias) {
-    const float logit = fmaf(a.scale, wave_sum(fmaf(q0, k0, q1 * k1)), bias);
-    const float top = fmaxf(m, logit), keep = m == top ? 1.0f : __expf(m - top), w = logit == top ? 1.0f : __expf(logit - top);
-    l = fmaf(l, keep, w);
-    o0 = fmaf(o0, keep, w * v0);
-    o1 = fmaf(o1, keep, w * v1);
-    m = top;
-  };
-  for (int i = wave; i < len; i += 4) {
-    const int64_t row = (int64_t)p * a.c.rows + i;
-    const float bias = a.beta ? a.beta[row] : 0.0f;
-    if (bias == -INFINITY) continue;
-    float k[8], v[8];
-    nunpack8(a.c.K[row * kNRow + lane], nscale(a.c.Ks[row] >> (8 * (lane >> 4)) & 255u), k);
-    nunpack8(a.c.V[row * kNRow + lane], nscale(a.c.Vs[row] >> (8 * (lane >> 4)) & 255u), v);
-    take(k[0], k[1], v[0], v[1], bias);
+namespace {
+
+// A pair's query planes, the scales of plane 0 as bytes, and the rows themselves as the tail's operands.
+template <int GP> struct Queries {
+  uint32_t plane[kAnPlanes][GP][kHeadDim / 4];
+  uint32_t scale[GP];
+  bf16x8 tail[4 * 64];
+};
+
+// Two channels a thread, 32 channels in 16 lanes of a row.  Queries beyond G are copies of the last.
+template <int W, int GP> __device__ inline void make_queries(const AttendN &a, int p, Queries<GP> &s) {
+  for (int i = threadIdx.x; i < GP * 64; i += 64 * W) {
+    const int q = i / 64, piece = i % 64;
+    const uint32_t w = reinterpret_cast<const uint32_t *>(a.Q + ((int64_t)p * a.G + min(q, a.G - 1)) * kHeadDim)[piece];
+    const float x[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+    uint32_t amax = max(__float_as_uint(x[0]) & 0x7fffffffu, __float_as_uint(x[1]) & 0x7fffffffu);
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
+    const bool finite = amax < 0x7f800000u;
+    // magnitudes below 2^(E + 1) at the type's end, below 2^E elsewhere; planes reach the least subnormal at the other
+    const int E = finite ? min(max((int)(amax >> 23) - 126, -111), 127) : 0;
+    float r[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) r[e] = finite ? ldexpf(x[e], -E) : 0.0f;
+#pragma unroll
+    for (int t = 0; t < kAnPlanes; ++t) {
+      const int c = __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], 0, false);
+      reinterpret_cast<uint16_t *>(s.plane[t][q])[piece] = (uint16_t)c;
+      const f32x2 got = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_pk_f32_fp8(c, false));
+#pragma unroll
+      for (int e = 0; e < 2; ++e) r[e] = (r[e] - got[e]) * 32.0f;
+    }
+    if (i % 16 == 0) reinterpret_cast<uint8_t *>(&s.scale[q])[piece / 16] = finite ? (uint8_t)(E + 127) : 255;
   }
-  for (int i = wave; i < len_f; i += 4) {
-    const int64_t at = ((int64_t)p * a.F + i) * kHeadDim + 2 * lane;
-    take((float)a.Kf[at], (float)a.Kf[at + 1], (float)a.Vf[at], (float)a.Vf[at + 1], 0.0f);
-  }
-  sO[wave][2 * lane] = o0;
-  sO[wave][2 * lane + 1] = o1;
-  if (lane == 0) {
-    sM[wave] = m;
-    sL[wave] = l;
-  }
-  __syncthreads();
-  if (threadIdx.x >= kHeadDim) return;
-  float M = -INFINITY, acc = 0.0f, sum = 0.0f;
-  for (int w = 0; w < 4; ++w) M = fmaxf(M, sM[w]);
-  for (int w = 0; w < 4; ++w) {
-    const float f = sM[w] == M ? 1.0f : __expf(sM[w] - M);
-    acc = fmaf(f, sO[w][threadIdx.x], acc);
-    sum = fmaf(f, sL[w], sum);
-  }
-  a.out[((int64_t)p * a.G + q) * kHeadDim + threadIdx.x] = sum == 0.0f ? 0.0f : acc / sum;
+  if (a.F > 0)
+    for (int i = threadIdx.x; i < 4 * 64; i += 64 * W) {
+      const int ks = i / 64, lane = i % 64, g = lane >> 4, r = lane & 15;
+      s.tail[i] = *reinterpret_cast<const bf16x8 *>(a.Q + ((int64_t)p * a.G + min(r % GP, a.G - 1)) * kHeadDim + 64 * (ks / 2) +
+                                                    16 * g + 8 * (ks % 2));
+    }
 }
 
-int attendn_chunks(int P, int rows, int F) { return 1; }
+// A wave's own part of LDS.  Rows stand in the order of the lanes that use them: row 16 kt + 4 j + g of a block, whose
+// logits are element j of the lanes of row g, at 16 kt + 4 g + j.
+template <int GP> struct WaveLds {
+  uint32_t ks[kAnBlock], vs[kAnBlock];
+  float bias[kAnBlock];
+  uint32_t p[GP < 16 ? 4 : 1][GP][4][8];   // [row g of lanes][query][term][tokens in pairs]; the fourth term is zero
+};
+
+// What a wave has in flight of a block.  Keys: row r' = 4 (r % 4) + r / 4 of each 16, so that element j of the logits of
+// lane row g is row 4 j + g and a load of values takes four whole rows in order.
+struct BlockData {
+  u32x4 k[4];        // lane (g, r): bytes 16 g .. 16 g + 15 of row 16 kt + r'
+  uint32_t v[16];    // bytes 4 r .. 4 r + 3 of row 16 (i / 4) + 4 (i % 4) + g
+  uint32_t ks, vs;   // of row `lane`
+  float bias;
+};
+
+template <bool BETA, int NT> __device__ inline void load_keys(const AttendN &a, int64_t row0, int live, BlockData &d) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const __amdgpu_buffer_rsrc_t kb = buffer(a.c.K + row0 * kNRow, live * kNRow);
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt)
+    d.k[kt] = __builtin_amdgcn_raw_buffer_load_b128(kb, (4 * (r & 3) + (r >> 2)) * kNRow + 16 * g, 16 * kNRow * kt, NT);
+  d.ks = __builtin_amdgcn_raw_buffer_load_b32(buffer(a.c.Ks + row0, live * 4), 4 * lane, 0, NT);
+  d.vs = __builtin_amdgcn_raw_buffer_load_b32(buffer(a.c.Vs + row0, live * 4), 4 * lane, 0, NT);
+  if constexpr (BETA)
+    d.bias = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(buffer(a.beta + row0, live * 4), 4 * lane, 0, 0));
+}
+
+template <int NT> __device__ inline void load_values(const AttendN &a, int64_t row0, int live, BlockData &d) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const __amdgpu_buffer_rsrc_t vb = buffer(a.c.V + row0 * kNRow, live * kNRow);
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    d.v[i] = __builtin_amdgcn_raw_buffer_load_b32(vb, g * kNRow + 4 * r, 4 * kNRow * i, NT);
+}
+
+// A float's bf16 terms: its upper half and the upper halves of what is left, one below the other.
+__device__ inline void terms(float x, uint32_t (&t)[3]) {
+  t[0] = __float_as_uint(x) & 0xffff0000u;
+  const float x1 = x - __uint_as_float(t[0]);
+  t[1] = __float_as_uint(x1) & 0xffff0000u;
+  t[2] = __float_as_uint(x1 - __uint_as_float(t[1]));
+}
+
+// The blocks first, first + W, ... below end, a wave's share of a chunk.
+template <int W, int GP, bool BETA, bool STREAM>
+__device__ inline void attend_blocks(const AttendN &a, int p, int first, int end, int len, const Queries<GP> &sq,
+                                     WaveLds<GP> &s, float &m, float &l, f32x4 (&o)[8]) {
+  constexpr int NT = STREAM ? kStreamed : 0;
+  constexpr int C = 16 / GP;                      // columns of a query
+  constexpr int NQ = kAnPlanes / C;               // products for its planes
+  constexpr int NP = (3 + C - 1) / C;             // and for its probabilities' terms
+  constexpr int N = 16 / C;                       // logits of a lane's share
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15, q = r % GP, part = r / GP;
+  const int place = (lane & 48) + 4 * (lane & 3) + ((lane & 15) >> 2);   // of row `lane` in LDS
+  const int64_t pr = (int64_t)p * a.c.rows;
+  auto live_at = [&](int idx) { return __builtin_amdgcn_readfirstlane(idx < end ? min(len - idx * kAnBlock, kAnBlock) : 0); };
+  int live = live_at(first);
+  BlockData d;
+  load_keys<BETA, NT>(a, pr + (int64_t)first * kAnBlock, live, d);
+  load_values<NT>(a, pr + (int64_t)first * kAnBlock, live, d);
+  // the planes of this lane's column: bytes 16 g .. and 64 + 16 g ..; one scale for channels 32 g ..
+  i32x8 qf[NQ];
+  int qscale[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int t = i * C + part;
+    const u32x4 lo = *reinterpret_cast<const u32x4 *>(&sq.plane[t][q][4 * g]), hi = *reinterpret_cast<const u32x4 *>(&sq.plane[t][q][16 + 4 * g]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      qf[i][e] = (int)lo[e];
+      qf[i][4 + e] = (int)hi[e];
+    }
+    const int byte = (int)(sq.scale[q] >> 8 * g & 255u);
+    qscale[i] = byte == 255 ? 255 : byte - 5 * t;
+  }
+  if constexpr (C > 1) {   // no fourth term
+    *reinterpret_cast<u32x4 *>(&s.p[g][q][3][0]) = u32x4{0u, 0u, 0u, 0u};
+    *reinterpret_cast<u32x4 *>(&s.p[g][q][3][4]) = u32x4{0u, 0u, 0u, 0u};
+  }
+  for (int idx = first; idx < end; idx += W) {
+    const int nlive = live_at(idx + W);
+    const int64_t next = pr + (int64_t)(nlive ? idx + W : idx) * kAnBlock;
+    {
+      const bool hidden = BETA && d.bias == -INFINITY;
+      s.ks[place] = d.ks;
+      s.vs[place] = hidden ? 0x7f7f7f7fu : d.vs;   // zero times NaN is not zero: a row left out is finite
+      if constexpr (BETA) s.bias[place] = lane < live ? d.bias : -INFINITY;
+    }
+    wave_exchange();
+    // ---- logits: rows 16 kt + 4 j + g of query q, a plane's part in each column
+    float sv[N];
+    {
+      f32x4 dots[4];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        i32x8 kf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          kf[e] = (int)d.k[kt][e];
+          kf[4 + e] = 0;
+        }
+        const int kscale = (int)reinterpret_cast<const uint8_t *>(s.ks)[4 * (16 * kt + r) + g];
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = NQ - 1; i >= 0; --i)
+          acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qf[i], acc, 4, 0, 0, kscale, 0, qscale[i]);
+        dots[kt] = acc;
+      }
+      // the planes' parts meet; each of the C copies of a column goes on with its own share of the rows
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (C >= 2) dots[kt][j] += from_lane<8>(dots[kt][j]);
+          if constexpr (C == 4) dots[kt][j] += from_lane<4>(dots[kt][j]);
+        }
+#pragma unroll
+      for (int t = 0; t < N / 4; ++t) {
+        f32x4 x = dots[t];
+#pragma unroll
+        for (int c = 1; c < C; ++c)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = part == c ? dots[c * (N / 4) + t][j] : x[j];
+        const int kt = part * (N / 4) + t;
+        if constexpr (BETA) {
+          const float4 b = *reinterpret_cast<const float4 *>(&s.bias[16 * kt + 4 * g]);
+          const float bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sv[4 * t + j] = bv[j] != -INFINITY ? fmaf(a.scale, x[j], bv[j]) : -INFINITY;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sv[4 * t + j] = 16 * kt + 4 * j + g < live ? a.scale * x[j] : -INFINITY;
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // the scales of this block's values leave LDS before the next block's come
+    u32x4 vs[4];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) vs[kt] = *reinterpret_cast<const u32x4 *>(&s.vs[16 * kt + 4 * g]);
+    if constexpr (W != kAnWide) load_keys<BETA, NT>(a, next, nlive, d);
+    __builtin_amdgcn_sched_barrier(0);
+    bool any;
+    float now;
+    const float keep = softmax_step<N, C, 0, false>(sv, m, l, any, now);
+    // ---- terms of the probabilities, to the lanes whose columns they are
+    Frag pf[NP][2];   // of tokens 0 .. 31 and 32 .. 63
+    if constexpr (C == 1) {
+      split_p(sv, pf[0][0], pf[1][0], pf[2][0]);
+      split_p(sv + 8, pf[0][1], pf[1][1], pf[2][1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        uint32_t t[4][3];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) terms(sv[4 * i + j], t[j]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          *reinterpret_cast<u32x2 *>(&s.p[g][q][k][2 * (part * (N / 4) + i)]) =
+              u32x2{upper_halves(t[0][k], t[1][k]), upper_halves(t[2][k], t[3][k])};
+      }
+      wave_exchange();
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          pf[i][h].v = *reinterpret_cast<const bf16x8 *>(&s.p[g][q][C * i + part][4 * h]);
+    }
+    // ---- (P V)^T: values as rows, one dim 8 r + e of the lane's tokens to each of eight operands
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[e][j] *= keep;
+    const int shift = 8 * (r >> 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      Frag vf[8];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int kt = 2 * h + w / 2, j = 2 * (w % 2);
+        const float s0 = __uint_as_float((vs[kt][j] >> shift & 255u) << 23), s1 = __uint_as_float((vs[kt][j + 1] >> shift & 255u) << 23);
+        const uint32_t x = d.v[4 * kt + j], y = d.v[4 * kt + j + 1];
+#define ARCKV_PAIR(b)                                                                                                   \
+  {                                                                                                                     \
+    const uint32_t xx = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s0, b)),              \
+                   yy = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y, s1, b));              \
+    vf[2 * b].w[w] = lower_halves(xx, yy);                                                                              \
+    vf[2 * b + 1].w[w] = upper_halves(xx, yy);                                                                          \
+  }
+        ARCKV_PAIR(0) ARCKV_PAIR(1) ARCKV_PAIR(2) ARCKV_PAIR(3)
+#undef ARCKV_PAIR
+      }
+#pragma unroll
+      for (int i = NP - 1; i >= 0; --i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = mfma16(vf[e].v, pf[i][h].v, o[e]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (W == kAnWide) return;   // its only block
+    load_values<NT>(a, next, nlive, d);
+    wave_exchange();   // the next block's scales and terms take the place of what was read here
+    __builtin_amdgcn_sched_barrier(0);
+    live = nlive;
+  }
+}
+
+// GP: the query rows that LDS and operands have room for, G <= GP <= 16.
+template <int W, int GP, bool BETA, bool STREAM>
+__global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 4) k_attendn_partial(AttendN a) {
+  constexpr int C = 16 / GP;
+  __shared__ __align__(16) Queries<GP> sQ;
+  union Own {
+    WaveLds<GP> work;
+    float o[GP][kHeadDim];   // in its place the wave's sums once they are complete
+  };
+  __shared__ __align__(16) Own sOwn[W];
+  __shared__ float sM[W][GP], sL[W][GP];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
+  const int ch = blockIdx.x, p = blockIdx.z * gridDim.y + blockIdx.y, G = a.G;
+  if (p >= a.c.P) return;
+  // units: blocks, then the tail's 32-row pieces; each chunk an equal share of those the pair has, wave by wave
+  const int len = clip_len(a.length, p, a.c.rows), len_f = clip_len(a.length_f, p, a.F);
+  const int blocks = (len + kAnBlock - 1) / kAnBlock, units = blocks + (len_f + kAttendTail - 1) / kAttendTail;
+  const int iters = W == kAnWide ? 1 : ((units + W - 1) / W + a.nch - 1) / a.nch;
+  const int first = ch * iters * W + wave, end = min(units, (ch + 1) * iters * W);
+  make_queries<W, GP>(a, p, sQ);
+  __syncthreads();
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o[8] = {};
+  const int bend = min(end, blocks);
+  if (first < bend) attend_blocks<W, GP, BETA, STREAM>(a, p, first, bend, len, sQ, sOwn[wave].work, m, l, o);
+  if (end > blocks) {
+    const int skip = first < blocks ? (blocks - first + W - 1) / W * W : 0;   // this wave's blocks
+    const int tfirst = first + skip - blocks, tend = end - blocks;
+    if (tfirst < tend) attend_tail<W, W == kAnWide, STREAM, GP>(a, p, tfirst, tend, len_f, sQ.tail, m, l, o);
+  }
+  // the terms' sums meet
+  if constexpr (C > 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o[e][j] += from_lane<8>(o[e][j]);
+        if constexpr (C == 4) o[e][j] += from_lane<4>(o[e][j]);
+      }
+  if (g == 0 && r < G) {
+    sM[wave][r] = m;
+    sL[wave][r] = l;
+  }
+  wave_exchange();
+  if (r < G)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float *to = &sOwn[wave].o[r][8 * (4 * g + j)];
+      *reinterpret_cast<float4 *>(to) = make_float4(o[0][j], o[1][j], o[2][j], o[3][j]);
+      *reinterpret_cast<float4 *>(to + 4) = make_float4(o[4][j], o[5][j], o[6][j], o[7][j]);
+    }
+  __syncthreads();
+  // one partial (max, sum, o) per query for the chunk; the result itself where there is one chunk
+  for (int idx = tid; idx < G * kHeadDim; idx += 64 * W) {
+    const int q = idx / kHeadDim, dim = idx % kHeadDim;
+    float M = sM[0][q];
+#pragma unroll
+    for (int w = 1; w < W; ++w) M = fmaxf(M, sM[w][q]);
+    const float ref = M == -INFINITY ? 0.0f : M;
+    float acc = 0.0f, lsum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = __expf(sM[w][q] - ref);   // a wave without a key in use: zero, as its sums are
+      acc = fmaf(f, sOwn[w].o[q][dim], acc);
+      lsum = fmaf(f, sL[w][q], lsum);
+    }
+    if (a.nch == 1) {
+      a.out[((int64_t)p * G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
+    } else {
+      const int64_t at = ((int64_t)p * a.nch + ch) * G + q;
+      a.part_o[at * kHeadDim + dim] = acc;
+      if (dim == 0) {
+        a.part_ml[2 * at] = M;
+        a.part_ml[2 * at + 1] = lsum;
+      }
+    }
+  }
+}
+
+int units_of(int rows, int F) { return (rows + kAnBlock - 1) / kAnBlock + (F + kAttendTail - 1) / kAttendTail; }
+
+// Whether a call is small: one wide workgroup per pair takes its units in one step, and no second launch joins what it
+// leaves.
+bool attendn_small(int P, int units) { return P <= 256 && units <= kAnWide; }
+
+}  // namespace
+
+// Chunks per pair.  Workgroups run kAnSlots at a time, so a call takes as many rounds as they fill, of a workgroup's units
+// and its start each; the number of chunks with the least sum is taken.
+int attendn_chunks(int P, int rows, int F) {
+  const int units = units_of(rows, F);
+  if (attendn_small(P, units)) return 1;
+  const int n = (units + kAnW - 1) / kAnW;
+  if ((int64_t)P * n <= kAnSlots) return n;
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int c = 1; c <= n && (int64_t)P * (c - 1) < 4 * kAnSlots; ++c) {
+    const int64_t cost = ((int64_t)P * c + kAnSlots - 1) / kAnSlots * ((n + c - 1) / c + kAnStart);
+    if (cost < least) {
+      least = cost;
+      best = c;
+    }
+  }
+  return best;
+}
 
 hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const void *Kf, const void *Vf, const int32_t *length_f, float *part_o,
                           float *part_ml, float *out, hipStream_t s) {
-  AttendN a{c, G, F, scale, (const bf16 *)Q, beta, length, (const bf16 *)Kf, (const bf16 *)Vf, length_f, part_o, part_ml, out};
+  AttendN a{c, G, F, scale, (const bf16 *)Q, beta, length, (const bf16 *)Kf, (const bf16 *)Vf, length_f, part_o, part_ml, out, 0};
+  a.nch = attendn_chunks(c.P, c.rows, F);
+  // pairs over y and z: a grid's y extent is limited
   const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
-  hipLaunchKernelGGL(k_attendn, dim3((unsigned)G, py, pz), dim3(256), 0, s, a);
+  const bool stream = (int64_t)c.P * c.rows * 2 * kNRow > kAnKept;
+  const bool small = attendn_small(c.P, units_of(c.rows, F));
+  auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py, pz), dim3(64 * (small ? kAnWide : kAnW)), 0, s, a);
+    return hipGetLastError();
+  };
+  auto by_stream = [&](auto gp, auto bt) {
+    constexpr int GP = decltype(gp)::value;
+    constexpr bool BETA = decltype(bt)::value;
+    if (small) return go(k_attendn_partial<kAnWide, GP, BETA, false>);
+    return stream ? go(k_attendn_partial<kAnW, GP, BETA, true>) : go(k_attendn_partial<kAnW, GP, BETA, false>);
+  };
+  auto by_beta = [&](auto gp) { return beta ? by_stream(gp, std::true_type{}) : by_stream(gp, std::false_type{}); };
+  const hipError_t e = G <= 4 ? by_beta(std::integral_constant<int, 4>{})
+                              : G <= 8 ? by_beta(std::integral_constant<int, 8>{}) : by_beta(std::integral_constant<int, 16>{});
+  if (e != hipSuccess || a.nch == 1) return e;
+  hipLaunchKernelGGL(k_attend_combine<AttendN>, dim3((unsigned)G, py, pz), dim3(kCombineGroups * kHeadDim), 0, s, a);
   return hipGetLastError();
 }
 

@@ -18,7 +18,7 @@
 //                      are loaded once this one's are used up, and so are its
 //                      values: 168 registers, three waves on a SIMD, 8 to 16 KB
 //                      in flight each.  The waves' (max, sum, o) are merged in LDS.
-//   k_attendq_combine  merges the partials of a pair; a call of one chunk per
+//   k_attend_combine  merges the partials of a pair; a call of one chunk per
 //                      pair needs none.
 // 512 pairs of 3277 int8 rows with bias and 256 tail rows take 74 us (6.6 TB/s; 77 us
 // with half lines of keys per load, 93 us with one block per wave and the tail in
@@ -26,7 +26,7 @@
 // 261 us (6.2 TB/s; 272, 314, 495).  Reading alone reaches 6.9 TB/s.
 #include <type_traits>
 
-#include "qcode.hpp"
+#include "attend_parts.hpp"
 
 namespace arckv {
 
@@ -35,37 +35,13 @@ constexpr int kAqW = 4;               // waves per workgroup
 constexpr int kAqWide = 16;           // of one that takes a whole pair of a small call, one unit per wave
 constexpr int kAqSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
 constexpr int kAqStart = 6;           // cost of a workgroup beside its blocks, in blocks per wave
-constexpr int kAqTail = 32;           // tail rows per wave
 // Bytes of codes above which keys and values are read as streams that the caches do not keep: a quarter of the last-level
 // cache, which a decode step's other layers pass through before a layer's turn comes again.  Three caches in turn, kept and
 // streamed (values alone): 64 pairs of 4096 rows (67 MB) 16.1 and 16.5 us, of 6000 23.5 and 22.7, of 8192 31.8 and 27.8.
 constexpr int64_t kAttendKept = (int64_t)64 << 20;
 
-__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
 __device__ inline f32x4 mfma16h(bf16x8 a, bf16x8 b, f32x4 c) {   // fp16 values in the fragments
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
-// LDS that only one wave uses: what its lanes wrote before is there for all of them (LDS takes a wave's accesses in order,
-// so this holds back the compiler alone).
-__device__ inline void wave_exchange() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-}
-
-union Frag {
-  uint32_t w[4];
-  bf16x8 v;
-};
-
-__device__ inline uint32_t upper_halves(uint32_t first, uint32_t second) {
-  return __builtin_amdgcn_perm(second, first, 0x07060302u);
-}
-__device__ inline uint32_t lower_halves(uint32_t first, uint32_t second) {
-  return __builtin_amdgcn_perm(second, first, 0x05040100u);
 }
 
 // Codes as MFMA operands, two to a word: four of a key as bf16 (the queries' type); those of four dims of two tokens
@@ -114,71 +90,6 @@ __device__ inline void split_p_f16(float p0, float p1, uint32_t &h, uint32_t &l)
   const f32x2 rest = {x[0] - (float)hi[0], x[1] - (float)hi[1]};
   h = __builtin_bit_cast(uint32_t, hi);
   l = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, f16x2));
-}
-
-// Probabilities of 8 keys as three bf16 terms (truncated, so all of one sign) that
-// sum to them exactly.
-__device__ inline void split_p(const float *p, Frag &h, Frag &m, Frag &l) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint32_t a[2], b[2], c[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float x = p[2 * k + i];
-      a[i] = __float_as_uint(x) & 0xffff0000u;
-      const float x1 = x - __uint_as_float(a[i]);
-      b[i] = __float_as_uint(x1) & 0xffff0000u;
-      c[i] = __float_as_uint(x1 - __uint_as_float(b[i]));
-    }
-    h.w[k] = upper_halves(a[0], a[1]);
-    m.w[k] = upper_halves(b[0], b[1]);
-    l.w[k] = upper_halves(c[0], c[1]);
-  }
-}
-
-// The word that lane r + FROM (mod 16) of the lane's row holds.
-template <int FROM> __device__ inline uint32_t from_lane(uint32_t x) {
-  return __builtin_amdgcn_update_dpp(0u, x, 0x120 + (16 - FROM), 0xf, 0xf, true);   // rotate right by 16 - FROM
-}
-template <int FROM> __device__ inline float from_lane(float x) { return __uint_as_float(from_lane<FROM>(__float_as_uint(x))); }
-
-// One step of a running softmax per query: turns the lane's N logits into probabilities times 2^SHIFT, takes them (without
-// 2^SHIFT) up in m and l, and returns what the earlier sums have to be multiplied by.  OWN: the probabilities are relative
-// to the step's own largest logit, which fp16 terms need where it lies far below the largest of all, and `now` is what this
-// step's sums have to be multiplied by; else they are relative to the new maximum and `now` is not used.  A query's logits lie
-// in the lanes of its column r of the four rows, and, PARTS > 1, of the columns r + 16 / PARTS, ....  -inf marks keys left
-// out; any: whether there is one that is not.
-template <int N, int PARTS, int SHIFT, bool OWN>
-__device__ inline float softmax_step(float (&sv)[N], float &m, float &l, bool &any, float &now) {
-  auto larger = [](float x, float y) { return fmaxf(x, y); };
-  auto plus = [](float x, float y) { return x + y; };
-  float top = sv[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) top = fmaxf(top, sv[i]);
-  if constexpr (PARTS == 4) top = fmaxf(top, from_lane<4>(top));
-  if constexpr (PARTS >= 2) top = fmaxf(top, from_lane<8>(top));
-  top = over_rows(top, larger);
-  any = top != -INFINITY;
-  const float own = any ? top : 0.0f;
-  top = fmaxf(top, m);
-  const float all = top == -INFINITY ? 0.0f : top, ref = OWN ? own : all;
-  const float keep = __builtin_amdgcn_exp2f((m - all) * 1.44269504f);
-  float sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    sv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i] - ref, 1.44269504f, (float)SHIFT));
-    sum += sv[i];
-  }
-  if constexpr (PARTS == 4) sum += from_lane<4>(sum);
-  if constexpr (PARTS >= 2) sum += from_lane<8>(sum);
-  sum = over_rows(sum, plus);
-  if constexpr (OWN) {
-    now = any ? __builtin_amdgcn_exp2f((own - all) * 1.44269504f) : 0.0f;
-    sum *= now;
-  }
-  m = top;
-  l = fmaf(l, keep, sum * (1.0f / (1 << SHIFT)));
-  return keep;
 }
 
 }  // namespace
@@ -420,78 +331,6 @@ __device__ inline void attend_blocks(const AttendQ &a, int p, int first, int end
   }
 }
 
-// 32 rows of the tail, `live` of them in use: what a wave has in flight of them.  The contraction steps are the blocks',
-// so a lane reads 32 bytes at a time of a key.
-__device__ inline void load_tail_keys(const AttendQ &a, int64_t row0, int live, u32x4 (&k)[2][4]) {
-  const int lane = threadIdx.x & 63, at = (lane & 15) * 2 * kHeadDim + 32 * (lane >> 4);
-  const __amdgpu_buffer_rsrc_t kb = buffer(a.Kf + row0 * kHeadDim, live * 2 * kHeadDim);
-#pragma unroll
-  for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
-      k[kt][ks] = __builtin_amdgcn_raw_buffer_load_b128(kb, at + 128 * (ks / 2) + 16 * (ks % 2), 32 * kHeadDim * kt, 0);
-}
-
-template <int NT> __device__ inline void load_tail_values(const AttendQ &a, int64_t row0, int live, u32x4 (&v)[8]) {
-  const int lane = threadIdx.x & 63, at = 4 * (lane >> 4) * 2 * kHeadDim + 16 * (lane & 15);
-  const __amdgpu_buffer_rsrc_t vb = buffer(a.Vf + row0 * kHeadDim, live * 2 * kHeadDim);
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    v[i] = __builtin_amdgcn_raw_buffer_load_b128(vb, at + 2 * kHeadDim * (i % 4), 32 * kHeadDim * (i / 4), NT);
-}
-
-// The tail's units of 32 rows first, first + W, ... below end, a wave's share of a chunk.
-template <int W, bool STREAM>
-__device__ inline void attend_tail(const AttendQ &a, int p, int first, int end, int len, const bf16x8 *s_q, float &m,
-                                   float &l, f32x4 (&o)[8]) {
-  constexpr int NTV = STREAM ? kStreamed : 0;
-  const int lane = threadIdx.x & 63, g = lane >> 4;
-  const int64_t pr = (int64_t)p * a.F;
-  auto live_at = [&](int idx) { return __builtin_amdgcn_readfirstlane(idx < end ? max(0, min(len - idx * kAqTail, kAqTail)) : 0); };
-  int live = live_at(first);
-  u32x4 k[2][4], v[8];
-  load_tail_keys(a, pr + first * kAqTail, live, k);
-  load_tail_values<NTV>(a, pr + first * kAqTail, live, v);
-  for (int idx = first; idx < end; idx += W) {
-    const int nlive = live_at(idx + W);
-    const int64_t next = pr + (idx + W) * kAqTail;
-    float sv[8];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) acc = mfma16(__builtin_bit_cast(bf16x8, k[kt][ks]), s_q[ks * 64 + lane], acc);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sv[4 * kt + j] = 16 * kt + 4 * g + j < live ? a.scale * acc[j] : -INFINITY;
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (W != kAqWide) load_tail_keys(a, next, nlive, k);
-    __builtin_amdgcn_sched_barrier(0);
-    bool any;
-    float now;
-    const float keep = softmax_step<8, 1, 0, false>(sv, m, l, any, now);
-    Frag ph, pm, pl;
-    split_p(sv, ph, pm, pl);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      Frag b;
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
-        b.w[n] = e & 1 ? upper_halves(v[2 * n][e / 2], v[2 * n + 1][e / 2]) : lower_halves(v[2 * n][e / 2], v[2 * n + 1][e / 2]);
-      // the first term has products of its own, which alone carry an infinite value (0 times it in the others is NaN)
-      const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-      const f32x4 lead = mfma16(b.v, ph.v, zero), rest = mfma16(b.v, pm.v, mfma16(b.v, pl.v, zero));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[e][j] = fmaf(o[e][j], keep, fabsf(lead[j]) < INFINITY ? lead[j] + rest[j] : lead[j]);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (W == kAqWide) return;
-    load_tail_values<NTV>(a, next, nlive, v);
-    __builtin_amdgcn_sched_barrier(0);
-    live = nlive;
-  }
-}
-
 // GP: the query rows that LDS and operands have room for, G <= GP <= 16.
 template <int W, int FMT, int GP, bool BETA, bool STREAM>
 __global__ void __launch_bounds__(64 * W, W == kAqW ? 3 : 4) k_attendq_partial(AttendQ a) {
@@ -527,8 +366,8 @@ __global__ void __launch_bounds__(64 * W, W == kAqW ? 3 : 4) k_attendq_partial(A
   if (end > a.nsel) {
     const int len_f = clip_len(a.length_f, p, a.F);
     const int skip = first < a.nsel ? (a.nsel - first + W - 1) / W * W : 0;   // this wave's blocks
-    const int tfirst = first + skip - a.nsel, tend = min(end - a.nsel, (len_f + kAqTail - 1) / kAqTail);
-    if (tfirst < tend) attend_tail<W, STREAM>(a, p, tfirst, tend, len_f, sOwn[wave].q, m, l, o);
+    const int tfirst = first + skip - a.nsel, tend = min(end - a.nsel, (len_f + kAttendTail - 1) / kAttendTail);
+    if (tfirst < tend) attend_tail<W, W == kAqWide, STREAM, 16>(a, p, tfirst, tend, len_f, sOwn[wave].q, m, l, o);
   }
   if (g == 0 && r < G) {
     sM[wave][r] = m;
@@ -570,64 +409,10 @@ __global__ void __launch_bounds__(64 * W, W == kAqW ? 3 : 4) k_attendq_partial(A
   }
 }
 
-// One workgroup per (query, pair): four groups of threads, thread = dim, take every fourth of the pair's partials, four
-// loads at a time, and meet in LDS: 86 chunks of 8 pairs take 4.2 us (9.8 us with one group).
-constexpr int kCombineGroups = 4, kCombineAhead = 4;
-__global__ void __launch_bounds__(kCombineGroups *kHeadDim) k_attendq_combine(AttendQ a) {
-  __shared__ float sM[kCombineGroups], sL[kCombineGroups], sA[kCombineGroups][kHeadDim];
-  const int q = blockIdx.x, dim = threadIdx.x % kHeadDim, group = threadIdx.x / kHeadDim, p = blockIdx.z * gridDim.y + blockIdx.y;
-  if (p >= a.c.P) return;
-  const float *ml = a.part_ml + ((int64_t)p * a.nch * a.G + q) * 2;
-  const float *po = a.part_o + ((int64_t)p * a.nch * a.G + q) * kHeadDim + dim;
-  float M = -INFINITY, lsum = 0.0f, acc = 0.0f;
-  for (int c0 = group; c0 < a.nch; c0 += kCombineGroups * kCombineAhead) {
-    float m[kCombineAhead], l[kCombineAhead], o[kCombineAhead], top = M;
-#pragma unroll
-    for (int i = 0; i < kCombineAhead; ++i) {
-      const int c = c0 + kCombineGroups * i;
-      const int64_t at = (int64_t)min(c, a.nch - 1) * a.G;
-      m[i] = ml[2 * at];
-      l[i] = ml[2 * at + 1];
-      o[i] = po[at * kHeadDim];
-      if (c >= a.nch) m[i] = -INFINITY, l[i] = o[i] = 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < kCombineAhead; ++i) top = fmaxf(top, m[i]);
-    const float ref = top == -INFINITY ? 0.0f : top, keep = __expf(M - ref);
-    lsum *= keep;
-    acc *= keep;
-#pragma unroll
-    for (int i = 0; i < kCombineAhead; ++i) {
-      const float f = __expf(m[i] - ref);   // a chunk without a key in use: zero, as its sums are
-      lsum = fmaf(f, l[i], lsum);
-      acc = fmaf(f, o[i], acc);
-    }
-    M = top;
-  }
-  if (dim == 0) {
-    sM[group] = M;
-    sL[group] = lsum;
-  }
-  sA[group][dim] = acc;
-  __syncthreads();
-  if (group) return;
-#pragma unroll
-  for (int i = 1; i < kCombineGroups; ++i) M = fmaxf(M, sM[i]);
-  const float ref = M == -INFINITY ? 0.0f : M;
-  acc = lsum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kCombineGroups; ++i) {
-    const float f = __expf(sM[i] - ref);
-    lsum = fmaf(f, sL[i], lsum);
-    acc = fmaf(f, sA[i][dim], acc);
-  }
-  a.out[((int64_t)p * a.G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
-}
-
 // Whether a call is small: one wide workgroup per pair takes its units in one step, and no second launch joins what it
 // leaves: 8 pairs of 819 + 37 rows take 10.5 us, 6.7 and 3.3 us in two launches, and 11.8 us a call against 15.9.
 static bool attendq_small(int P, int nsel, int F) {
-  return P <= 256 && nsel + (F + kAqTail - 1) / kAqTail <= kAqWide;
+  return P <= 256 && nsel + (F + kAttendTail - 1) / kAttendTail <= kAqWide;
 }
 
 // Chunks per pair, and the units (blocks and 32-row pieces of the tail) per wave of one.  Workgroups run kAqSlots at a
@@ -635,7 +420,7 @@ static bool attendq_small(int P, int nsel, int F) {
 // the least sum is taken: 512 pairs of 3277 + 256 rows in one chunk each took 80 us where three took 96; 8192 to 16384
 // rows go in three.
 int attendq_chunks(int P, int nsel, int F, int *iters) {
-  const int units = nsel + (F + kAqTail - 1) / kAqTail;
+  const int units = nsel + (F + kAttendTail - 1) / kAttendTail;
   if (attendq_small(P, nsel, F)) {
     *iters = 1;
     return 1;
@@ -686,7 +471,7 @@ hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, c
   const hipError_t e = fmt == ARCKV_E4M3 ? by_rows(std::integral_constant<int, ARCKV_E4M3>{})
                                          : by_rows(std::integral_constant<int, ARCKV_INT8>{});
   if (e != hipSuccess || a.nch == 1) return e;
-  hipLaunchKernelGGL(k_attendq_combine, dim3((unsigned)G, py, pz), dim3(kCombineGroups * kHeadDim), 0, s, a);
+  hipLaunchKernelGGL(k_attend_combine<AttendQ>, dim3((unsigned)G, py, pz), dim3(kCombineGroups * kHeadDim), 0, s, a);
   return hipGetLastError();
 }
 

@@ -8,6 +8,7 @@ of the compaction: if the library is missing, loading fails loudly.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import NamedTuple, Optional
@@ -683,11 +684,15 @@ def ncache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bflo
     return K, V
 
 
-def attend_ncache_workspace_size(P: int, rows: int, G: int, F: int = 0) -> int:
+@functools.lru_cache(maxsize=256)          # of sizes alone; the call takes a tenth of a decode step's host time
+def _attend_ncache_ws(P: int, rows: int, G: int, F: int) -> int:
     out = ctypes.c_size_t()
-    args = [_int32(x, what) for x, what in ((P, "P"), (rows, "rows"), (G, "G"), (F, "F"))]
-    _check(lib().arckv_attend_ncache_workspace_size(*args, ctypes.byref(out)), "arckv_attend_ncache_workspace_size")
+    _check(lib().arckv_attend_ncache_workspace_size(P, rows, G, F, ctypes.byref(out)), "arckv_attend_ncache_workspace_size")
     return out.value
+
+
+def attend_ncache_workspace_size(P: int, rows: int, G: int, F: int = 0) -> int:
+    return _attend_ncache_ws(_int32(P, "P"), _int32(rows, "rows"), _int32(G, "G"), _int32(F, "F"))
 
 
 def attend_ncache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f=None, scale=None, out=None,
@@ -707,10 +712,7 @@ def attend_ncache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f
     else:
         optr = _qptr(out, whole, torch.float32, dev, "out")
     if ws is None:
-        nbytes = ctypes.c_size_t()
-        _check(lib().arckv_attend_ncache_workspace_size(P, rows, G, F, ctypes.byref(nbytes)),
-               "arckv_attend_ncache_workspace_size")
-        nbytes = nbytes.value
+        nbytes = _attend_ncache_ws(P, rows, G, F)
         # torch's device allocations are 512-byte aligned
         ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
         wptr = ws.data_ptr() if nbytes else None
@@ -744,18 +746,20 @@ def rotary_frequencies(d_rot: int = 128, base: float = 10000.0, mode: str = "non
 def _rotary_rows(x, y, N: int, dtype, dev: int, what: str) -> RotaryRows:
     """x [N][heads][128] into y, both with any strides of tokens and heads."""
     shape = x.shape
-    for t, name in ((x, what), (y, what + "'s output")):
-        if t.dtype is not dtype:
-            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-        if len(shape) != 3 or shape[0] != N or shape[2] != 128 or t.shape != shape:
-            raise ValueError(f"{name}: expected shape ({N}, heads, 128), got {tuple(t.shape)}")
-        if t.stride(2) != 1:
-            raise ValueError(f"{name}: a row's channels must be contiguous")
-    if x.get_device() != dev or y.get_device() != dev:
+    # one chain where all is well: a decode step's call checks four tensors
+    if not (x.dtype is dtype and y.dtype is dtype and len(shape) == 3 and shape[0] == N and shape[2] == 128
+            and y.shape == shape and x.get_device() == dev == y.get_device()):
+        for t, name in ((x, what), (y, what + "'s output")):
+            if t.dtype is not dtype:
+                raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+            if len(shape) != 3 or shape[0] != N or shape[2] != 128 or t.shape != shape:
+                raise ValueError(f"{name}: expected shape ({N}, heads, 128), got {tuple(t.shape)}")
         raise ValueError(f"{what}: tensors must live on the current GPU")
     heads = shape[1]
-    xt, xh, _ = x.stride()
-    yt, yh, _ = y.stride()
+    xt, xh, xc = x.stride()
+    yt, yh, yc = y.stride()
+    if xc != 1 or yc != 1:
+        raise ValueError(f"{what}: a row's channels must be contiguous")
     if N == 1:              # the stride of an axis of one says nothing
         xt = yt = 0
     if heads == 1:

@@ -17,23 +17,16 @@ __device__ inline int nscale_exp(uint32_t amax_bits) {
 // A scale byte as a number: 2^(byte - 127), NaN for 255 (0, which no write leaves, is 0).
 __device__ inline float nscale(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(byte << 23); }
 
-// Eight numbers to codes: e2m1 of x / scale, to nearest even, magnitudes above 6 to 6.
+// Four numbers to codes: e2m1 of x / scale, to nearest even, magnitudes above 6 to 6; eight.
+__device__ inline uint32_t npack4(float a, float b, float c, float d, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(__builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, a, b, scale, 0), c, d, scale, 1);
+}
 __device__ inline uint32_t npack8(const float *x, float scale) {
   uint32_t w = 0;
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
-}
-
-// And back: scale * code, which is exact.
-__device__ inline void nunpack8(uint32_t w, float scale, float *x) {
-  f32x2 v[4] = {__builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0)),
-                __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1)),
-                __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2)),
-                __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3))};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = v[i / 2][i % 2];
 }
 
 }  // namespace arckv

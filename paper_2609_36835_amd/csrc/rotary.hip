@@ -1,23 +1,151 @@
 // Rotary positions: pairs of channels turned by position * frequency.
 //
-// One workgroup per token, a thread a pair of channels; the angle's sine and cosine serve all heads.
+// HBM-bound: every row is read and written once.  A row is cut into pieces of 16 bytes, and a thread takes the two that
+// belong together (channels c .. and c + half .., or neighbours) of four rows, all loaded before the angles are formed: a
+// workgroup's rows follow each other through tokens and heads, so it needs the angles of few tokens, each formed once, by one
+// thread, for all heads, and handed out through LDS.
 #include "common.hpp"
+#include "qcode.hpp"
 #include "rotary.hpp"
 
 namespace arckv {
 
-template <typename T> __global__ void __launch_bounds__(256) k_rotary(Rotary a) {
+namespace {
+constexpr int kRotRows = 4;        // of a thread
+constexpr int kRotThreads = 256;
+// Bytes above which rows are read as streams that the caches do not keep: 4096 tokens of 40 heads (42 MB in) take 14.1 us kept
+// and 14.8 streamed, 32768 tokens (336 MB) 125.5 and 122.8, 262144 of two heads (134 MB) 63.5 and 59.5.
+constexpr int64_t kRotKept = (int64_t)64 << 20;
+template <typename T> constexpr int kRotPer = 16 / (int)sizeof(T);                     // channels of a piece
+template <typename T> constexpr int kRotSlots = kRotThreads * 2 * kRotPer<T> / kHeadDim;  // rows that threads take at a time
+template <typename T> constexpr int kRotTile = kRotSlots<T> * kRotRows;                // and a workgroup in all
+
+// Turns per position of a pair.
+__device__ inline double turns_of(const Rotary &a, int i) { return a.freq[i] * 0.15915494309189533577; }
+
+__device__ inline void angle(const Rotary &a, int64_t n, double per_position, float &c, float &s) {
+  // whole turns leave in float64: a position has up to 31 bits and the angle's remainder needs 24 more
+  const double turns = (double)(a.positions ? a.positions[n] : (int)n) * per_position;
+  sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+  s *= a.sign * a.factor;
+  c *= a.factor;
+}
+
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  __device__ static inline void unpack(u32x4 w, float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
+  }
+  __device__ static inline u32x4 pack(const float (&x)[4]) {
+    return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+  }
+};
+template <> struct Piece<bf16> {
+  __device__ static inline void unpack(u32x4 w, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+  }
+  __device__ static inline u32x4 pack(const float (&x)[8]) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)x[2 * e], (bf16)x[2 * e + 1]});
+    return w;
+  }
+};
+
+}  // namespace
+
+template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bounds__(kRotThreads) k_rotary(Rotary a) {
+  constexpr int PER = kRotPer<T>, THREADS = kHeadDim / (2 * PER), SLOTS = kRotSlots<T>, TILE = kRotTile<T>;
+  extern __shared__ __align__(16) float s_angle[];   // [token][cos, sin][64]
+  const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int H = a.heads[0] + a.heads[1];
+  const int64_t row0 = block * TILE, rows = (int64_t)a.N * H;
+  if (row0 >= rows) return;
+  const int64_t n0 = H == 1 ? row0 : row0 / H;
+  const int first = (int)(row0 - n0 * H), count = (int)min((int64_t)TILE, rows - row0);   // row of token n0; rows of this workgroup
+  const int c = threadIdx.x % THREADS, slot = threadIdx.x / THREADS;
+  // the thread's pieces: of pairs (halves), of neighbouring channels, or two that are copied; neighbouring threads have
+  // neighbouring pieces, so that streamed stores fill lines
+  const int turned = NEIGHBOURS ? 2 * a.half / PER : a.half / PER;
+  const bool pairs = !NEIGHBOURS && c < turned;
+  const int pu = NEIGHBOURS || pairs ? c : c + turned, pv = NEIGHBOURS ? c + THREADS : pairs ? c + turned : c + THREADS;
+  u32x4 u[kRotRows], v[kRotRows];
+  T *y[kRotRows];
+  int token[kRotRows];
+#pragma unroll
+  for (int k = 0; k < kRotRows; ++k) {
+    const int i = min(slot + SLOTS * k, count - 1) + first;   // rows past the end load the last one and store nothing
+    // i < TILE + H: a token further at most where H is a tile or more, else exact for i < 2 TILE
+    token[k] = H >= TILE ? (i >= H) : (int)(((uint32_t)i * a.by_heads) >> 16);
+    const int h = i - token[k] * H, t = h >= a.heads[0];
+    const RotaryRows &r = a.r[t];
+    const int64_t n = n0 + token[k], hh = h - (t ? a.heads[0] : 0);
+    const T *x = (const T *)r.x + n * r.x_token + hh * r.x_head;
+    y[k] = (T *)r.y + n * r.y_token + hh * r.y_head;
+    if constexpr (STREAM) {
+      u[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + pu * PER));
+      v[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + pv * PER));
+    } else {
+      u[k] = *reinterpret_cast<const u32x4 *>(x + pu * PER);
+      v[k] = *reinterpret_cast<const u32x4 *>(x + pv * PER);
+    }
+  }
+  const int last = (count - 1 + first) / H;
+  const int f = threadIdx.x % 64;
+  if (f < a.half) {
+    const double per_position = turns_of(a, f);
+    for (int t = threadIdx.x / 64; t <= last; t += kRotThreads / 64)
+      angle(a, n0 + t, per_position, s_angle[t * 128 + f], s_angle[t * 128 + 64 + f]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kRotRows; ++k) {
+    const float *cs = s_angle + token[k] * 128;
+    if (pairs) {
+      float xu[PER], xv[PER], yu[PER], yv[PER];
+      Piece<T>::unpack(u[k], xu);
+      Piece<T>::unpack(v[k], xv);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const float co = cs[PER * c + e], si = cs[64 + PER * c + e];
+        yu[e] = xu[e] * co - xv[e] * si;
+        yv[e] = xu[e] * si + xv[e] * co;
+      }
+      u[k] = Piece<T>::pack(yu);
+      v[k] = Piece<T>::pack(yv);
+    }
+    if constexpr (NEIGHBOURS) {
+      auto turn = [&](u32x4 &w, int piece) {
+        if (piece >= turned) return;
+        float x[PER], z[PER];
+        Piece<T>::unpack(w, x);
+#pragma unroll
+        for (int e = 0; e < PER / 2; ++e) {
+          const float co = cs[PER / 2 * piece + e], si = cs[64 + PER / 2 * piece + e];
+          z[2 * e] = x[2 * e] * co - x[2 * e + 1] * si;
+          z[2 * e + 1] = x[2 * e] * si + x[2 * e + 1] * co;
+        }
+        w = Piece<T>::pack(z);
+      };
+      turn(u[k], pu);
+      turn(v[k], pv);
+    }
+    if (slot + SLOTS * k < count) {
+      __builtin_nontemporal_store(u[k], reinterpret_cast<u32x4 *>(y[k] + pu * PER));
+      __builtin_nontemporal_store(v[k], reinterpret_cast<u32x4 *>(y[k] + pv * PER));
+    }
+  }
+}
+
+// Pairs that do not fill whole pieces: one workgroup per token, a thread a pair of channels.
+template <typename T> __global__ void __launch_bounds__(256) k_rotary_pairs(Rotary a) {
   const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (n >= a.N) return;
   const int i = threadIdx.x % 64;   // a pair, or two channels behind the pairs
   float c = 1.0f, s = 0.0f;
-  if (i < a.half) {
-    // whole turns leave in float64: a position has up to 31 bits and the angle's remainder needs 24 more
-    const double turns = (double)(a.positions ? a.positions[n] : (int)n) * a.freq[i] * 0.15915494309189533577;
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-    s *= a.sign * a.factor;
-    c *= a.factor;
-  }
+  if (i < a.half) angle(a, n, turns_of(a, i), c, s);
   const int u = i < a.half ? (a.neighbours ? 2 * i : i) : 2 * i, v = i < a.half && !a.neighbours ? i + a.half : u + 1;
   for (int h = threadIdx.x / 64; h < a.heads[0] + a.heads[1]; h += 4) {
     const int t = h >= a.heads[0], hh = h - (t ? a.heads[0] : 0);
@@ -30,13 +158,29 @@ template <typename T> __global__ void __launch_bounds__(256) k_rotary(Rotary a) 
   }
 }
 
+template <typename T> static hipError_t launch_rotary_of(Rotary a, hipStream_t s) {
+  const int H = a.heads[0] + a.heads[1];
+  if ((a.neighbours ? 2 * a.half : a.half) % kRotPer<T> != 0) {
+    const dim3 grid((unsigned)min(a.N, 65536), (unsigned)((a.N + 65535) / 65536));
+    hipLaunchKernelGGL(k_rotary_pairs<T>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  constexpr int TILE = kRotTile<T>;
+  a.by_heads = (65536 + H - 1) / H;   // used below TILE heads: exact for i < 2 TILE <= 256
+  const int64_t blocks = ((int64_t)a.N * H + TILE - 1) / TILE;
+  const dim3 grid((unsigned)min(blocks, (int64_t)65536), (unsigned)((blocks + 65535) / 65536));
+  const int tokens = min(a.N, H == 1 ? TILE : (TILE + H - 2) / H + 1);
+  auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), tokens * 128 * sizeof(float), s, a);
+    return hipGetLastError();
+  };
+  const bool stream = (int64_t)a.N * H * kHeadDim * (int)sizeof(T) > kRotKept;
+  if (a.neighbours) return stream ? go(k_rotary<T, true, true>) : go(k_rotary<T, true, false>);
+  return stream ? go(k_rotary<T, false, true>) : go(k_rotary<T, false, false>);
+}
+
 hipError_t launch_rotary(int dtype, const Rotary &a, hipStream_t s) {
-  const dim3 grid((unsigned)min(a.N, 65536), (unsigned)((a.N + 65535) / 65536));
-  if (dtype == ARCKV_BF16)
-    hipLaunchKernelGGL(k_rotary<bf16>, grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(k_rotary<float>, grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+  return dtype == ARCKV_BF16 ? launch_rotary_of<bf16>(a, s) : launch_rotary_of<float>(a, s);
 }
 
 }  // namespace arckv

@@ -18,6 +18,7 @@ struct Rotary {
   float sign, factor;        // -1 turns back
   const int32_t *positions;  // or null
   const double *freq;
+  uint32_t by_heads;         // 2^16 / heads, rounded up
 };
 
 }  // namespace arckv

@@ -583,7 +583,7 @@ typedef struct {
 /*   positions [N] int32 device array, any sign, or NULL: token n is at position n;
  *   freq      [d_rot / 2] float64 device array, radians per position;
  *   a, b      rows that share the positions (a layer's queries and keys); b may be NULL.
- * Tensors 16-byte aligned.  No workspace, no synchronisation. */
+ * Tensors 16-byte aligned, at most 2^30 rows in all.  No workspace, no synchronisation. */
 arckv_status arckv_rotary(const arckv_rotary_params *p, const int32_t *positions, const double *freq,
                           const arckv_rotary_rows *a, const arckv_rotary_rows *b, hipStream_t stream);
 

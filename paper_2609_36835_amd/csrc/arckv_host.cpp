@@ -1190,6 +1190,7 @@ arckv_status arckv_attend_ncache(const arckv_ncache *c, int32_t G, int32_t F, fl
 // ---------------------------------------------------------------- rotary positions
 constexpr int32_t kRotaryTokensMax = 1 << 26;
 constexpr int32_t kRotaryHeadsMax = 1 << 20;
+constexpr int64_t kRotaryRowsMax = (int64_t)1 << 30;     // in all: 256 GiB of bf16 out
 constexpr int64_t kRotaryStrideMax = (int64_t)1 << 34;   // elements; offsets stay below 2^60
 
 static arckv_status check_rotary_rows(const arckv_rotary_rows *r, int32_t N, int width) {
@@ -1223,6 +1224,7 @@ arckv_status arckv_rotary(const arckv_rotary_params *p, const int32_t *positions
   const int width = p->dtype == ARCKV_F32 ? 4 : 2;
   CHECK(check_rotary_rows(a, p->N, width));
   if (b) CHECK(check_rotary_rows(b, p->N, width));
+  if ((int64_t)p->N * (a->heads + (b ? b->heads : 0)) > kRotaryRowsMax) return ARCKV_ERR_UNSUPPORTED;
   Rotary r{};
   const arckv_rotary_rows *rows[2] = {a, b};
   for (int i = 0; i < 2; ++i)

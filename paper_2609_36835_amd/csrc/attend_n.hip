@@ -34,6 +34,9 @@ constexpr int kAnWide = 16;           // of one that takes a whole pair of a sma
 constexpr int kAnSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
 constexpr int kAnStart = 6;           // cost of a workgroup beside its units, in units per wave
 constexpr int kAnPlanes = 4;
+// How far logits may pass the reference of their exponentials: probabilities stay below 2^8, and sums are rescaled a few
+// times in a call instead of at every block.
+constexpr float kAnLag = 5.5451774f;
 // Bytes above which codes are read as streams that the caches do not keep.
 constexpr int64_t kAnKept = (int64_t)64 << 20;
 
@@ -98,7 +101,8 @@ template <int W, int GP> __device__ inline void make_queries(const AttendN &a, i
 // A wave's own part of LDS.  Rows stand in the order of the lanes that use them: row 16 kt + 4 j + g of a block, whose
 // logits are element j of the lanes of row g, at 16 kt + 4 g + j.
 template <int GP> struct WaveLds {
-  uint32_t ks[kAnBlock], vs[kAnBlock];
+  uint32_t ks[kAnBlock];                   // four scale bytes
+  float vs[kHeadDim / kNGroup][kAnBlock];  // scales of a group as numbers
   float bias[kAnBlock];
   uint32_t p[GP < 16 ? 4 : 1][GP][4][8];   // [row g of lanes][query][term][tokens in pairs]; the fourth term is zero
 };
@@ -140,6 +144,14 @@ __device__ inline void terms(float x, uint32_t (&t)[3]) {
   t[2] = __float_as_uint(x1 - __uint_as_float(t[1]));
 }
 
+// Two dims (byte B of x and y) of two tokens as bf16, scales included, dim by dim.
+template <int B> __device__ inline void value_pairs(uint32_t x, uint32_t y, float sx, float sy, uint32_t &even, uint32_t &odd) {
+  const uint32_t xx = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, sx, B)),
+                 yy = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y, sy, B));
+  even = lower_halves(xx, yy);
+  odd = upper_halves(xx, yy);
+}
+
 // The blocks first, first + W, ... below end, a wave's share of a chunk.
 template <int W, int GP, bool BETA, bool STREAM>
 __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end, int len, const Queries<GP> &sq,
@@ -160,17 +172,23 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
   // the planes of this lane's column: bytes 16 g .. and 64 + 16 g ..; one scale for channels 32 g ..
   i32x8 qf[NQ];
   int qscale[NQ];
+  auto load_planes = [&] {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const u32x4 *plane = reinterpret_cast<const u32x4 *>(&sq.plane[i * C + part][q][4 * g]);
+      const u32x4 lo = plane[0], hi = plane[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        qf[i][e] = (int)lo[e];
+        qf[i][4 + e] = (int)hi[e];
+      }
+    }
+  };
+  if constexpr (NQ == 1) load_planes();   // more of them stay in LDS
 #pragma unroll
   for (int i = 0; i < NQ; ++i) {
-    const int t = i * C + part;
-    const u32x4 lo = *reinterpret_cast<const u32x4 *>(&sq.plane[t][q][4 * g]), hi = *reinterpret_cast<const u32x4 *>(&sq.plane[t][q][16 + 4 * g]);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      qf[i][e] = (int)lo[e];
-      qf[i][4 + e] = (int)hi[e];
-    }
     const int byte = (int)(sq.scale[q] >> 8 * g & 255u);
-    qscale[i] = byte == 255 ? 255 : byte - 5 * t;
+    qscale[i] = byte == 255 ? 255 : byte - 5 * (i * C + part);
   }
   if constexpr (C > 1) {   // no fourth term
     *reinterpret_cast<u32x4 *>(&s.p[g][q][3][0]) = u32x4{0u, 0u, 0u, 0u};
@@ -180,12 +198,17 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
     const int nlive = live_at(idx + W);
     const int64_t next = pr + (int64_t)(nlive ? idx + W : idx) * kAnBlock;
     {
-      const bool hidden = BETA && d.bias == -INFINITY;
+      // zero times NaN is not zero: a row left out is finite.  (255, a NaN's byte, becomes an infinity, which converts to NaN.)
+      const uint32_t vs = BETA && d.bias == -INFINITY ? 0x7f7f7f7fu : d.vs;
       s.ks[place] = d.ks;
-      s.vs[place] = hidden ? 0x7f7f7f7fu : d.vs;   // zero times NaN is not zero: a row left out is finite
+      s.vs[0][place] = __uint_as_float((vs & 255u) << 23);
+      s.vs[1][place] = __uint_as_float((vs >> 8 & 255u) << 23);
+      s.vs[2][place] = __uint_as_float((vs >> 16 & 255u) << 23);
+      s.vs[3][place] = __uint_as_float(vs >> 24 << 23);
       if constexpr (BETA) s.bias[place] = lane < live ? d.bias : -INFINITY;
     }
     wave_exchange();
+    if constexpr (NQ > 1) load_planes();
     // ---- logits: rows 16 kt + 4 j + g of query q, a plane's part in each column
     float sv[N];
     {
@@ -234,14 +257,36 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
     }
     __builtin_amdgcn_sched_barrier(0);
     // the scales of this block's values leave LDS before the next block's come
-    u32x4 vs[4];
+    f32x4 vs[4];
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) vs[kt] = *reinterpret_cast<const u32x4 *>(&s.vs[16 * kt + 4 * g]);
+    for (int kt = 0; kt < 4; ++kt) vs[kt] = *reinterpret_cast<const f32x4 *>(&s.vs[r >> 2][16 * kt + 4 * g]);
     if constexpr (W != kAnWide) load_keys<BETA, NT>(a, next, nlive, d);
     __builtin_amdgcn_sched_barrier(0);
-    bool any;
-    float now;
-    const float keep = softmax_step<N, C, 0, false>(sv, m, l, any, now);
+    // ---- probabilities relative to a reference m, which follows the maximum only when that has left it far behind
+    {
+      float top = sv[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) top = fmaxf(top, sv[i]);
+      if (__any(top > m + kAnLag)) {
+        auto larger = [](float x, float y) { return fmaxf(x, y); };
+        if constexpr (C == 4) top = fmaxf(top, from_lane<4>(top));
+        if constexpr (C >= 2) top = fmaxf(top, from_lane<8>(top));
+        top = fmaxf(over_rows(top, larger), m);
+        const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * 1.44269504f);
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[e][j] *= keep;
+        m = top;
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        sv[i] = __builtin_amdgcn_exp2f((sv[i] - ref) * 1.44269504f);
+        l += sv[i];
+      }
+    }
     // ---- terms of the probabilities, to the lanes whose columns they are
     Frag pf[NP][2];   // of tokens 0 .. 31 and 32 .. 63
     if constexpr (C == 1) {
@@ -267,40 +312,34 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
     }
     // ---- (P V)^T: values as rows, one dim 8 r + e of the lane's tokens to each of eight operands
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[e][j] *= keep;
-    const int shift = 8 * (r >> 2);
+      for (int eh = 0; eh < 2; ++eh) {
+        Frag vf[4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      Frag vf[8];
+        for (int w = 0; w < 4; ++w) {
+          const int kt = 2 * h + w / 2, j = 2 * (w % 2);
+          eh ? value_pairs<2>(d.v[4 * kt + j], d.v[4 * kt + j + 1], vs[kt][j], vs[kt][j + 1], vf[0].w[w], vf[1].w[w])
+             : value_pairs<0>(d.v[4 * kt + j], d.v[4 * kt + j + 1], vs[kt][j], vs[kt][j + 1], vf[0].w[w], vf[1].w[w]);
+          eh ? value_pairs<3>(d.v[4 * kt + j], d.v[4 * kt + j + 1], vs[kt][j], vs[kt][j + 1], vf[2].w[w], vf[3].w[w])
+             : value_pairs<1>(d.v[4 * kt + j], d.v[4 * kt + j + 1], vs[kt][j], vs[kt][j + 1], vf[2].w[w], vf[3].w[w]);
+        }
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int kt = 2 * h + w / 2, j = 2 * (w % 2);
-        const float s0 = __uint_as_float((vs[kt][j] >> shift & 255u) << 23), s1 = __uint_as_float((vs[kt][j + 1] >> shift & 255u) << 23);
-        const uint32_t x = d.v[4 * kt + j], y = d.v[4 * kt + j + 1];
-#define ARCKV_PAIR(b)                                                                                                   \
-  {                                                                                                                     \
-    const uint32_t xx = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s0, b)),              \
-                   yy = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y, s1, b));              \
-    vf[2 * b].w[w] = lower_halves(xx, yy);                                                                              \
-    vf[2 * b + 1].w[w] = upper_halves(xx, yy);                                                                          \
-  }
-        ARCKV_PAIR(0) ARCKV_PAIR(1) ARCKV_PAIR(2) ARCKV_PAIR(3)
-#undef ARCKV_PAIR
+        for (int i = NP - 1; i >= 0; --i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[4 * eh + e] = mfma16(vf[e].v, pf[i][h].v, o[4 * eh + e]);
       }
-#pragma unroll
-      for (int i = NP - 1; i >= 0; --i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = mfma16(vf[e].v, pf[i][h].v, o[e]);
-    }
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (W == kAnWide) return;   // its only block
+    if constexpr (W == kAnWide) break;   // its only block
     load_values<NT>(a, next, nlive, d);
     wave_exchange();   // the next block's scales and terms take the place of what was read here
     __builtin_amdgcn_sched_barrier(0);
     live = nlive;
   }
+  // each lane's share of the sum of probabilities meets the others
+  if constexpr (C == 4) l += from_lane<4>(l);
+  if constexpr (C >= 2) l += from_lane<8>(l);
+  l = over_rows(l, [](float x, float y) { return x + y; });
 }
 
 // GP: the query rows that LDS and operands have room for, G <= GP <= 16.

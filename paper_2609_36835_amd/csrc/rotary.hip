@@ -1,9 +1,9 @@
 // Rotary positions: pairs of channels turned by position * frequency.
 //
 // HBM-bound: every row is read and written once.  A row is cut into pieces of 16 bytes, and a thread takes the two that
-// belong together (channels c .. and c + half .., or neighbours) of four rows, all loaded before the angles are formed: a
-// workgroup's rows follow each other through tokens and heads, so it needs the angles of few tokens, each formed once, by one
-// thread, for all heads, and handed out through LDS.
+// belong together (channels c .. and c + half .., or neighbours) of one row or four, all loaded before the angles are
+// formed: a workgroup's rows follow each other through tokens and heads, so it needs the angles of few tokens, each formed
+// once, by one thread, for all its heads, and handed out through LDS.
 #include "common.hpp"
 #include "qcode.hpp"
 #include "rotary.hpp"
@@ -11,14 +11,14 @@
 namespace arckv {
 
 namespace {
-constexpr int kRotRows = 4;        // of a thread
 constexpr int kRotThreads = 256;
 // Bytes above which rows are read as streams that the caches do not keep: 4096 tokens of 40 heads (42 MB in) take 14.1 us kept
 // and 14.8 streamed, 32768 tokens (336 MB) 125.5 and 122.8, 262144 of two heads (134 MB) 63.5 and 59.5.
 constexpr int64_t kRotKept = (int64_t)64 << 20;
+template <bool STREAM> constexpr int kRotRows = STREAM ? 1 : 4;   // of a thread: 113.0 and 123.1 us streamed, 16.1 and 14.1 kept
 template <typename T> constexpr int kRotPer = 16 / (int)sizeof(T);                     // channels of a piece
 template <typename T> constexpr int kRotSlots = kRotThreads * 2 * kRotPer<T> / kHeadDim;  // rows that threads take at a time
-template <typename T> constexpr int kRotTile = kRotSlots<T> * kRotRows;                // and a workgroup in all
+template <typename T, bool STREAM> constexpr int kRotTile = kRotSlots<T> * kRotRows<STREAM>;   // and a workgroup in all
 
 // Turns per position of a pair.
 __device__ inline double turns_of(const Rotary &a, int i) { return a.freq[i] * 0.15915494309189533577; }
@@ -57,7 +57,7 @@ template <> struct Piece<bf16> {
 }  // namespace
 
 template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bounds__(kRotThreads) k_rotary(Rotary a) {
-  constexpr int PER = kRotPer<T>, THREADS = kHeadDim / (2 * PER), SLOTS = kRotSlots<T>, TILE = kRotTile<T>;
+  constexpr int PER = kRotPer<T>, THREADS = kHeadDim / (2 * PER), SLOTS = kRotSlots<T>, ROWS = kRotRows<STREAM>, TILE = kRotTile<T, STREAM>;
   extern __shared__ __align__(16) float s_angle[];   // [token][cos, sin][64]
   const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   const int H = a.heads[0] + a.heads[1];
@@ -71,11 +71,11 @@ template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bou
   const int turned = NEIGHBOURS ? 2 * a.half / PER : a.half / PER;
   const bool pairs = !NEIGHBOURS && c < turned;
   const int pu = NEIGHBOURS || pairs ? c : c + turned, pv = NEIGHBOURS ? c + THREADS : pairs ? c + turned : c + THREADS;
-  u32x4 u[kRotRows], v[kRotRows];
-  T *y[kRotRows];
-  int token[kRotRows];
+  u32x4 u[ROWS], v[ROWS];
+  T *y[ROWS];
+  int token[ROWS];
 #pragma unroll
-  for (int k = 0; k < kRotRows; ++k) {
+  for (int k = 0; k < ROWS; ++k) {
     const int i = min(slot + SLOTS * k, count - 1) + first;   // rows past the end load the last one and store nothing
     // i < TILE + H: a token further at most where H is a tile or more, else exact for i < 2 TILE
     token[k] = H >= TILE ? (i >= H) : (int)(((uint32_t)i * a.by_heads) >> 16);
@@ -101,7 +101,7 @@ template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bou
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kRotRows; ++k) {
+  for (int k = 0; k < ROWS; ++k) {
     const float *cs = s_angle + token[k] * 128;
     if (pairs) {
       float xu[PER], xv[PER], yu[PER], yv[PER];
@@ -165,18 +165,18 @@ template <typename T> static hipError_t launch_rotary_of(Rotary a, hipStream_t s
     hipLaunchKernelGGL(k_rotary_pairs<T>, grid, dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  constexpr int TILE = kRotTile<T>;
-  a.by_heads = (65536 + H - 1) / H;   // used below TILE heads: exact for i < 2 TILE <= 256
-  const int64_t blocks = ((int64_t)a.N * H + TILE - 1) / TILE;
-  const dim3 grid((unsigned)min(blocks, (int64_t)65536), (unsigned)((blocks + 65535) / 65536));
-  const int tokens = min(a.N, H == 1 ? TILE : (TILE + H - 2) / H + 1);
-  auto go = [&](auto kern) {
+  a.by_heads = (65536 + H - 1) / H;   // used where H is below a workgroup's rows: exact for i < TILE + H
+  auto go = [&](auto kern, int64_t tile) {
+    const int64_t blocks = ((int64_t)a.N * H + tile - 1) / tile;
+    const dim3 grid((unsigned)min(blocks, (int64_t)65536), (unsigned)((blocks + 65535) / 65536));
+    const int64_t tokens = min((int64_t)a.N, H == 1 ? tile : (tile + H - 2) / H + 1);
     hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), tokens * 128 * sizeof(float), s, a);
     return hipGetLastError();
   };
   const bool stream = (int64_t)a.N * H * kHeadDim * (int)sizeof(T) > kRotKept;
-  if (a.neighbours) return stream ? go(k_rotary<T, true, true>) : go(k_rotary<T, true, false>);
-  return stream ? go(k_rotary<T, false, true>) : go(k_rotary<T, false, false>);
+  if (a.neighbours)
+    return stream ? go(k_rotary<T, true, true>, kRotTile<T, true>) : go(k_rotary<T, true, false>, kRotTile<T, false>);
+  return stream ? go(k_rotary<T, false, true>, kRotTile<T, true>) : go(k_rotary<T, false, false>, kRotTile<T, false>);
 }
 
 hipError_t launch_rotary(int dtype, const Rotary &a, hipStream_t s) {

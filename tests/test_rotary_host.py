@@ -103,6 +103,9 @@ def test_rotary_refuses():
     for kw, want in bad:
         assert f(params(), None, FAKE, rows(**kw), None, None) == want, kw
         assert f(params(), None, FAKE, rows(), rows(**kw), None) == want, kw
+    many = dict(heads=1 << 10, xt=1 << 18, yt=1 << 18)
+    assert f(params(N=(1 << 20) + 1), None, FAKE, rows(**many), None, None) == A.ERR_UNSUPPORTED
+    assert f(params(N=1 << 20), None, FAKE, rows(**many), rows(), None) == A.ERR_UNSUPPORTED
 
 
 @needs_no_gpu

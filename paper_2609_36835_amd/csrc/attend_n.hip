@@ -32,7 +32,6 @@ constexpr int kAnBlock = 64;          // rows of a unit
 constexpr int kAnW = 4;               // waves per workgroup
 constexpr int kAnWide = 16;           // of one that takes a whole pair of a small call, one unit per wave
 constexpr int kAnSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
-constexpr int kAnStart = 6;           // cost of a workgroup beside its units, in units per wave
 constexpr int kAnPlanes = 4;
 // How far logits may pass the reference of their exponentials: probabilities stay below 2^8, and sums are rescaled a few
 // times in a call instead of at every block.
@@ -152,10 +151,10 @@ template <int B> __device__ inline void value_pairs(uint32_t x, uint32_t y, floa
   odd = upper_halves(xx, yy);
 }
 
-// The blocks first, first + W, ... below end, a wave's share of a chunk.
+// The blocks first, first + W, ... below end, a wave's share of a chunk, the first of them on its way in d.
 template <int W, int GP, bool BETA, bool STREAM>
 __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end, int len, const Queries<GP> &sq,
-                                     WaveLds<GP> &s, float &m, float &l, f32x4 (&o)[8]) {
+                                     WaveLds<GP> &s, BlockData &d, float &m, float &l, f32x4 (&o)[8]) {
   constexpr int NT = STREAM ? kStreamed : 0;
   constexpr int C = 16 / GP;                      // columns of a query
   constexpr int NQ = kAnPlanes / C;               // products for its planes
@@ -166,9 +165,6 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
   const int64_t pr = (int64_t)p * a.c.rows;
   auto live_at = [&](int idx) { return __builtin_amdgcn_readfirstlane(idx < end ? min(len - idx * kAnBlock, kAnBlock) : 0); };
   int live = live_at(first);
-  BlockData d;
-  load_keys<BETA, NT>(a, pr + (int64_t)first * kAnBlock, live, d);
-  load_values<NT>(a, pr + (int64_t)first * kAnBlock, live, d);
   // the planes of this lane's column: bytes 16 g .. and 64 + 16 g ..; one scale for channels 32 g ..
   i32x8 qf[NQ];
   int qscale[NQ];
@@ -361,12 +357,21 @@ __global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 4) k_attendn_partial(A
   const int blocks = (len + kAnBlock - 1) / kAnBlock, units = blocks + (len_f + kAttendTail - 1) / kAttendTail;
   const int iters = W == kAnWide ? 1 : ((units + W - 1) / W + a.nch - 1) / a.nch;
   const int first = ch * iters * W + wave, end = min(units, (ch + 1) * iters * W);
+  const int bend = min(end, blocks);
+  BlockData d;
+  if (first < bend) {   // on their way while the queries are made ready
+    constexpr int NT = STREAM ? kStreamed : 0;
+    const int64_t row0 = (int64_t)p * a.c.rows + (int64_t)first * kAnBlock;
+    const int live = __builtin_amdgcn_readfirstlane(min(len - first * kAnBlock, kAnBlock));
+    load_keys<BETA, NT>(a, row0, live, d);
+    load_values<NT>(a, row0, live, d);
+    __builtin_amdgcn_sched_barrier(0);
+  }
   make_queries<W, GP>(a, p, sQ);
   __syncthreads();
   float m = -INFINITY, l = 0.0f;
   f32x4 o[8] = {};
-  const int bend = min(end, blocks);
-  if (first < bend) attend_blocks<W, GP, BETA, STREAM>(a, p, first, bend, len, sQ, sOwn[wave].work, m, l, o);
+  if (first < bend) attend_blocks<W, GP, BETA, STREAM>(a, p, first, bend, len, sQ, sOwn[wave].work, d, m, l, o);
   if (end > blocks) {
     const int skip = first < blocks ? (blocks - first + W - 1) / W * W : 0;   // this wave's blocks
     const int tfirst = first + skip - blocks, tend = end - blocks;
@@ -429,17 +434,22 @@ bool attendn_small(int P, int units) { return P <= 256 && units <= kAnWide; }
 
 }  // namespace
 
-// Chunks per pair.  Workgroups run kAnSlots at a time, so a call takes as many rounds as they fill, of a workgroup's units
-// and its start each; the number of chunks with the least sum is taken.
+// Chunks per pair, by the time that a call of as many takes, in ns: up to three workgroups run at a time on each of 256 CUs
+// (the fullest ends the call), which share the memory's rate but need a wave's latency for each unit all the same; a
+// workgroup's start; the second launch, which joins.
+// us per call by chunks: 512 pairs of 3277 + 256 rows 1: 50.3, 2: 52.5, 3: 53.9; of 8192-16384 rows 1: 139.5, 2: 148.8, 3: 145.5; 8
+// pairs of 131072 rows 21: 41.7, 32: 34.7, 43: 36.2, 64: 33.0, 86: 35.7; 64 pairs of 1500 rows 1: 10.0, 2: 14.2, 6: 14.0.
 int attendn_chunks(int P, int rows, int F) {
+  constexpr int64_t kCus = 256, kLatency = 1300, kShare = 1400, kStart = 3000, kJoin = 6000, kJoinChunk = 50;
   const int units = units_of(rows, F);
   if (attendn_small(P, units)) return 1;
   const int n = (units + kAnW - 1) / kAnW;
-  if ((int64_t)P * n <= kAnSlots) return n;
   int best = 1;
   int64_t least = INT64_MAX;
-  for (int c = 1; c <= n && (int64_t)P * (c - 1) < 4 * kAnSlots; ++c) {
-    const int64_t cost = ((int64_t)P * c + kAnSlots - 1) / kAnSlots * ((n + c - 1) / c + kAnStart);
+  for (int c = 1; c <= n && (int64_t)P * (c - 1) < 2 * kAnSlots; ++c) {
+    const int64_t wgs = (int64_t)P * c, rounds = (wgs + kAnSlots - 1) / kAnSlots;
+    const int64_t unit = max(kLatency, kShare * min((wgs + kCus - 1) / kCus, kAnSlots / kCus));
+    const int64_t cost = rounds * ((n + c - 1) / c * unit + kStart) + (c > 1 ? kJoin + kJoinChunk * c : 0);
     if (cost < least) {
       least = cost;
       best = c;
@@ -471,7 +481,10 @@ hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void
   const hipError_t e = G <= 4 ? by_beta(std::integral_constant<int, 4>{})
                               : G <= 8 ? by_beta(std::integral_constant<int, 8>{}) : by_beta(std::integral_constant<int, 16>{});
   if (e != hipSuccess || a.nch == 1) return e;
-  hipLaunchKernelGGL(k_attend_combine<AttendN>, dim3((unsigned)G, py, pz), dim3(kCombineGroups * kHeadDim), 0, s, a);
+  if (a.nch <= kCombineAhead)   // one group's loads
+    hipLaunchKernelGGL((k_attend_combine<AttendN, 1>), dim3((unsigned)G, py, pz), dim3(kHeadDim), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_attend_combine<AttendN, kCombineGroups>), dim3((unsigned)G, py, pz), dim3(kCombineGroups * kHeadDim), 0, s, a);
   return hipGetLastError();
 }
 

@@ -178,18 +178,18 @@ __device__ inline void attend_tail(const A &a, int p, int first, int end, int le
 // One workgroup per (query, pair): four groups of threads, thread = dim, take every fourth of the pair's partials, four
 // loads at a time, and meet in LDS: 86 chunks of 8 pairs take 4.2 us (9.8 us with one group).
 constexpr int kCombineGroups = 4, kCombineAhead = 4;
-template <typename A> __global__ void __launch_bounds__(kCombineGroups *kHeadDim) k_attend_combine(A a) {
-  __shared__ float sM[kCombineGroups], sL[kCombineGroups], sA[kCombineGroups][kHeadDim];
+template <typename A, int GROUPS> __global__ void __launch_bounds__(GROUPS *kHeadDim) k_attend_combine(A a) {
+  __shared__ float sM[GROUPS], sL[GROUPS], sA[GROUPS][kHeadDim];
   const int q = blockIdx.x, dim = threadIdx.x % kHeadDim, group = threadIdx.x / kHeadDim, p = blockIdx.z * gridDim.y + blockIdx.y;
   if (p >= a.c.P) return;
   const float *ml = a.part_ml + ((int64_t)p * a.nch * a.G + q) * 2;
   const float *po = a.part_o + ((int64_t)p * a.nch * a.G + q) * kHeadDim + dim;
   float M = -INFINITY, lsum = 0.0f, acc = 0.0f;
-  for (int c0 = group; c0 < a.nch; c0 += kCombineGroups * kCombineAhead) {
+  for (int c0 = group; c0 < a.nch; c0 += GROUPS * kCombineAhead) {
     float m[kCombineAhead], l[kCombineAhead], o[kCombineAhead], top = M;
 #pragma unroll
     for (int i = 0; i < kCombineAhead; ++i) {
-      const int c = c0 + kCombineGroups * i;
+      const int c = c0 + GROUPS * i;
       const int64_t at = (int64_t)min(c, a.nch - 1) * a.G;
       m[i] = ml[2 * at];
       l[i] = ml[2 * at + 1];
@@ -209,6 +209,10 @@ template <typename A> __global__ void __launch_bounds__(kCombineGroups *kHeadDim
     }
     M = top;
   }
+  if constexpr (GROUPS == 1) {
+    a.out[((int64_t)p * a.G + q) * kHeadDim + dim] = lsum == 0.0f ? 0.0f : acc / lsum;
+    return;
+  }
   if (dim == 0) {
     sM[group] = M;
     sL[group] = lsum;
@@ -217,11 +221,11 @@ template <typename A> __global__ void __launch_bounds__(kCombineGroups *kHeadDim
   __syncthreads();
   if (group) return;
 #pragma unroll
-  for (int i = 1; i < kCombineGroups; ++i) M = fmaxf(M, sM[i]);
+  for (int i = 1; i < GROUPS; ++i) M = fmaxf(M, sM[i]);
   const float ref = M == -INFINITY ? 0.0f : M;
   acc = lsum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kCombineGroups; ++i) {
+  for (int i = 0; i < GROUPS; ++i) {
     const float f = __expf(sM[i] - ref);
     lsum = fmaf(f, sL[i], lsum);
     acc = fmaf(f, sA[i][dim], acc);

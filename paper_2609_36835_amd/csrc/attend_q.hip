@@ -471,7 +471,7 @@ hipError_t launch_attendq(int fmt, const QCache &c, int G, int F, float scale, c
   const hipError_t e = fmt == ARCKV_E4M3 ? by_rows(std::integral_constant<int, ARCKV_E4M3>{})
                                          : by_rows(std::integral_constant<int, ARCKV_INT8>{});
   if (e != hipSuccess || a.nch == 1) return e;
-  hipLaunchKernelGGL(k_attend_combine<AttendQ>, dim3((unsigned)G, py, pz), dim3(kCombineGroups * kHeadDim), 0, s, a);
+  hipLaunchKernelGGL((k_attend_combine<AttendQ, kCombineGroups>), dim3((unsigned)G, py, pz), dim3(kCombineGroups * kHeadDim), 0, s, a);
   return hipGetLastError();
 }
 

@@ -36,8 +36,9 @@ constexpr int kAnPlanes = 4;
 // How far logits may pass the reference of their exponentials: probabilities stay below 2^8, and sums are rescaled a few
 // times in a call instead of at every block.
 constexpr float kAnLag = 5.5451774f;
-// Bytes above which codes are read as streams that the caches do not keep.
-constexpr int64_t kAnKept = (int64_t)64 << 20;
+// Bytes above which codes are read as streams that the caches do not keep: 64 pairs of 8192 rows (71 MB) take 18.2 us kept and
+// 19.2 streamed, of 12000 24.8 and 24.5, of 16384 31.7 and 29.2, three caches in turn.
+constexpr int64_t kAnKept = (int64_t)96 << 20;
 
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 }  // namespace

@@ -2,6 +2,8 @@
 (every refusal comes before any HIP call) and of the binding."""
 import ctypes
 import math
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -151,3 +153,26 @@ def test_the_cache_has_the_documented_arrays():
     c = A.ncache(3, 70, device="cpu")
     assert [tuple(t.shape) for t in c] == [(3, 70, 64), (3, 70, 64), (3, 70, 4), (3, 70, 4)]
     assert all(t.dtype == torch.uint8 for t in c)
+
+
+@needs_no_gpu
+def test_host_code_under_sanitizers():
+    """Refusals, workspace sizes and frequencies under AddressSanitizer and UndefinedBehaviorSanitizer (no GPU)."""
+    from paper_2609_36835_amd import build as B
+    from tests.test_host_sanitizers import HOST_SAN, OUT, PKG, ROOT, _kernel_objects
+    objs = _kernel_objects()
+    if not objs:
+        pytest.skip("kernel objects not built (run paper_2609_36835_amd.build first)")
+    os.makedirs(OUT, exist_ok=True)
+    hipcc, inc = B._hipcc(), ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG, "csrc")]
+    host_o, drv_o, exe = (os.path.join(OUT, n) for n in ("arckv_host_nc.o", "ncache_checks.o", "ncache_checks"))
+    for cmd in ([hipcc, "-std=c++17", "-fPIC", *HOST_SAN, *inc, "-c", os.path.join(PKG, "csrc", "arckv_host.cpp"), "-o", host_o],
+                [hipcc, "-std=c++17", *HOST_SAN, *inc, "-c", os.path.join(ROOT, "tests", "sanitize", "ncache_checks.cpp"),
+                 "-o", drv_o],
+                [hipcc, f"--offload-arch={B.ARCH}", *HOST_SAN, drv_o, host_o, *objs, "-o", exe]):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        assert r.returncode == 0, (" ".join(cmd), r.stderr[-4000:])
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:halt_on_error=1",
+               UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1", HIP_VISIBLE_DEVICES="")
+    r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
+    assert r.returncode == 0 and "ok: 0 failures" in r.stdout, (r.stdout[-4000:], r.stderr[-4000:])

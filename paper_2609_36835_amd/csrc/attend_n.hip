@@ -33,9 +33,10 @@ constexpr int kAnW = 4;               // waves per workgroup
 constexpr int kAnWide = 16;           // of one that takes a whole pair of a small call, one unit per wave
 constexpr int kAnSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
 constexpr int kAnPlanes = 4;
-// How far logits may pass the reference of their exponentials: probabilities stay below 2^8, and sums are rescaled a few
-// times in a call instead of at every block.
-constexpr float kAnLag = 5.5451774f;
+// How far the reference of the exponentials is set above the largest logit when one passes it: probabilities stay below 1 (so
+// that large values do not overflow beside them) and the largest above 2^-8 or so, and sums are rescaled a few times in a call
+// instead of at every block.
+constexpr float kAnLead = 5.5451774f;
 // Bytes above which codes are read as streams that the caches do not keep: 64 pairs of 8192 rows (71 MB) take 18.2 us kept and
 // 19.2 streamed, of 12000 24.8 and 24.5, of 16384 31.7 and 29.2, three caches in turn.
 constexpr int64_t kAnKept = (int64_t)96 << 20;
@@ -259,23 +260,23 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
     for (int kt = 0; kt < 4; ++kt) vs[kt] = *reinterpret_cast<const f32x4 *>(&s.vs[r >> 2][16 * kt + 4 * g]);
     if constexpr (W != kAnWide) load_keys<BETA, NT>(a, next, nlive, d);
     __builtin_amdgcn_sched_barrier(0);
-    // ---- probabilities relative to a reference m, which follows the maximum only when that has left it far behind
+    // ---- probabilities relative to a reference m at or above every logit so far
     {
       float top = sv[0];
 #pragma unroll
       for (int i = 1; i < N; ++i) top = fmaxf(top, sv[i]);
-      if (__any(top > m + kAnLag)) {
+      if (__any(top > m)) {
         auto larger = [](float x, float y) { return fmaxf(x, y); };
         if constexpr (C == 4) top = fmaxf(top, from_lane<4>(top));
         if constexpr (C >= 2) top = fmaxf(top, from_lane<8>(top));
-        top = fmaxf(over_rows(top, larger), m);
-        const float keep = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * 1.44269504f);
+        top = over_rows(top, larger);
+        const float to = top > m ? top + kAnLead : m, keep = m == to ? 1.0f : __builtin_amdgcn_exp2f((m - to) * 1.44269504f);
         l *= keep;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[e][j] *= keep;
-        m = top;
+        m = to;
       }
       const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll

@@ -356,6 +356,27 @@ def test_attend_far_logits(order, G):
     check_attend(A().attend_ncache(Q, c, beta), Q, c, beta, None, None, None, None)
 
 
+@pytest.mark.parametrize("G", [3, 8, 16])
+def test_attend_largest_values(G):
+    """Rows of the largest magnitude, many of them of equal weight, or one behind others: a finite mean."""
+    P, R = 3, 200
+    big = 6 * 2.0 ** 125
+    K, V = torch.zeros(P, R, 128, device="cuda"), torch.full((P, R, 128), 3.3e38, device="cuda")
+    V[1, :, ::2] = -3.3e38
+    V[2, :R - 1] = 1.0
+    b = torch.zeros(P, R, device="cuda")
+    b[2] = torch.linspace(-30, 30, R)
+    c = make_cache(P, R)
+    A().ncache_write(c, K, V)
+    Q = torch.ones(P, G, 128, dtype=torch.bfloat16, device="cuda")
+    out = np64(A().attend_ncache(Q, c, b))
+    sign = np.where(np.arange(128) % 2 == 0, -1, 1)
+    tol = 2 * (2.0 ** -21 + 12 * R * U) * big
+    assert (np.abs(out[0] - big) <= tol).all() and (np.abs(out[1] - big * sign) <= tol).all()
+    w = np.exp(np64(b[2]) - 30)
+    assert (np.abs(out[2] - (w[-1] * big + w[:-1].sum()) / w.sum()) <= tol).all()
+
+
 def test_attend_small_and_large_query_channels():
     """Query channels over the whole range beside a large one; keys are such that each part shows."""
     g = np.random.default_rng(14)

@@ -651,11 +651,17 @@ def ncache(P: int, rows: int, device="cuda") -> NCache:
 def _ncache(c) -> tuple:
     """(struct, P, rows, current device) of a cache tuple."""
     K, V, Ks, Vs = c
-    dev = torch.cuda.current_device()
-    P, rows, width = K.shape
-    codes, scales, u8 = (P, rows, 64), (P, rows, 4), torch.uint8
-    return NCacheStruct(P, rows, 128, _qptr(K, codes, u8, dev, "K"), _qptr(V, codes, u8, dev, "V"),
-                        _qptr(Ks, scales, u8, dev, "K_scale"), _qptr(Vs, scales, u8, dev, "V_scale")), P, rows, dev
+    dev, u8, codes = torch.cuda.current_device(), torch.uint8, K.shape
+    P, rows, width = codes
+    scales = (P, rows, 4)
+    # one chain where all is well: a fifth of a decode step's host time
+    if not (width == 64 and V.shape == codes and Ks.shape == scales and Vs.shape == scales
+            and K.dtype is u8 and V.dtype is u8 and Ks.dtype is u8 and Vs.dtype is u8
+            and K.get_device() == dev and V.get_device() == dev and Ks.get_device() == dev and Vs.get_device() == dev
+            and K.is_contiguous() and V.is_contiguous() and Ks.is_contiguous() and Vs.is_contiguous()):
+        for x, shape, what in ((K, (P, rows, 64), "K"), (V, (P, rows, 64), "V"), (Ks, scales, "K_scale"), (Vs, scales, "V_scale")):
+            _qptr(x, shape, u8, dev, what)
+    return NCacheStruct(P, rows, 128, K.data_ptr(), V.data_ptr(), Ks.data_ptr(), Vs.data_ptr()), P, rows, dev
 
 
 def ncache_write(cache, K, V, start=None, count=None) -> None:
@@ -707,7 +713,7 @@ def attend_ncache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f
     row, tail, whole, i32, bf16 = (P,), (P, F, 128), (P, G, 128), torch.int32, torch.bfloat16
     qptr = _qptr(Q, whole, bf16, dev, "Q")
     if out is None:
-        out = torch.empty(whole, dtype=torch.float32, device=Q.device)
+        out = Q.new_empty(whole, dtype=torch.float32)
         optr = out.data_ptr()
     else:
         optr = _qptr(out, whole, torch.float32, dev, "out")

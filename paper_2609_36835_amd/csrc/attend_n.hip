@@ -440,9 +440,10 @@ bool attendn_small(int P, int units) { return P <= 256 && units <= kAnWide; }
 // (the fullest ends the call), which share the memory's rate but need a wave's latency for each unit all the same; a
 // workgroup's start; the second launch, which joins.
 // us per call by chunks: 512 pairs of 3277 + 256 rows 1: 50.3, 2: 52.5, 3: 53.9; of 8192-16384 rows 1: 139.5, 2: 148.8, 3: 145.5; 8
-// pairs of 131072 rows 21: 41.7, 32: 34.7, 43: 36.2, 64: 33.0, 86: 35.7; 64 pairs of 1500 rows 1: 10.0, 2: 14.2, 6: 14.0.
+// pairs of 131072 rows 21: 41.7, 32: 34.7, 43: 36.2, 64: 33.0, 86: 35.7; 32 of 85005 8: 68.3, 16: 65.8, 24: 64.4; 256 of 4500-9000
+// 1: 51.7, 2: 47.3, 3: 45.6; 64 of 1500 1: 10.0, 2: 14.2, 6: 14.0.
 int attendn_chunks(int P, int rows, int F) {
-  constexpr int64_t kCus = 256, kLatency = 1300, kShare = 1400, kStart = 3000, kJoin = 6000, kJoinChunk = 50;
+  constexpr int64_t kCus = 256, kAlone = 1300, kLatency = 1600, kShare = 1400, kStart = 3000, kJoin = 6000, kJoinChunk = 50;
   const int units = units_of(rows, F);
   if (attendn_small(P, units)) return 1;
   const int n = (units + kAnW - 1) / kAnW;
@@ -450,7 +451,7 @@ int attendn_chunks(int P, int rows, int F) {
   int64_t least = INT64_MAX;
   for (int c = 1; c <= n && (int64_t)P * (c - 1) < 2 * kAnSlots; ++c) {
     const int64_t wgs = (int64_t)P * c, rounds = (wgs + kAnSlots - 1) / kAnSlots;
-    const int64_t unit = max(kLatency, kShare * min((wgs + kCus - 1) / kCus, kAnSlots / kCus));
+    const int64_t unit = wgs <= kCus / 2 ? kAlone : max(kLatency, kShare * min((wgs + kCus - 1) / kCus, kAnSlots / kCus));
     const int64_t cost = rounds * ((n + c - 1) / c * unit + kStart) + (c > 1 ? kJoin + kJoinChunk * c : 0);
     if (cost < least) {
       least = cost;

@@ -3,7 +3,8 @@
 // HBM-bound: every row is read and written once.  A row is cut into pieces of 16 bytes, and a thread takes the two that
 // belong together (channels c .. and c + half .., or neighbours) of one row or four, all loaded before the angles are
 // formed: a workgroup's rows follow each other through tokens and heads, so it needs the angles of few tokens, each formed
-// once, by one thread, for all its heads, and handed out through LDS.
+// once, by one thread, for all its heads, and handed out through LDS.  Halves that end inside a piece have their rows in LDS
+// too, where a channel finds its mate at any distance.
 #include "common.hpp"
 #include "qcode.hpp"
 #include "rotary.hpp"
@@ -56,9 +57,12 @@ template <> struct Piece<bf16> {
 
 }  // namespace
 
-template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bounds__(kRotThreads) k_rotary(Rotary a) {
+enum RotaryMode { kHalves, kNeighbours, kUnevenHalves };
+
+template <typename T, int MODE, bool STREAM> __global__ void __launch_bounds__(kRotThreads) k_rotary(Rotary a) {
   constexpr int PER = kRotPer<T>, THREADS = kHeadDim / (2 * PER), SLOTS = kRotSlots<T>, ROWS = kRotRows<STREAM>, TILE = kRotTile<T, STREAM>;
   extern __shared__ __align__(16) float s_angle[];   // [token][cos, sin][64]
+  __shared__ __align__(16) T s_row[MODE == kUnevenHalves ? TILE : 1][kHeadDim];
   const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   const int H = a.heads[0] + a.heads[1];
   const int64_t row0 = block * TILE, rows = (int64_t)a.N * H;
@@ -66,11 +70,11 @@ template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bou
   const int64_t n0 = H == 1 ? row0 : row0 / H;
   const int first = (int)(row0 - n0 * H), count = (int)min((int64_t)TILE, rows - row0);   // row of token n0; rows of this workgroup
   const int c = threadIdx.x % THREADS, slot = threadIdx.x / THREADS;
-  // the thread's pieces: of pairs (halves), of neighbouring channels, or two that are copied; neighbouring threads have
-  // neighbouring pieces, so that streamed stores fill lines
-  const int turned = NEIGHBOURS ? 2 * a.half / PER : a.half / PER;
-  const bool pairs = !NEIGHBOURS && c < turned;
-  const int pu = NEIGHBOURS || pairs ? c : c + turned, pv = NEIGHBOURS ? c + THREADS : pairs ? c + turned : c + THREADS;
+  // the thread's pieces: two that are pairs (halves), any two (of neighbours, of a row in LDS), or two that are copied;
+  // neighbouring threads have neighbouring pieces, so that streamed stores fill lines
+  const int turned = a.half / PER;
+  const bool pairs = MODE == kHalves && c < turned;
+  const int pu = MODE != kHalves || pairs ? c : c + turned, pv = pairs ? c + turned : c + THREADS;
   u32x4 u[ROWS], v[ROWS];
   T *y[ROWS];
   int token[ROWS];
@@ -90,6 +94,10 @@ template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bou
     } else {
       u[k] = *reinterpret_cast<const u32x4 *>(x + pu * PER);
       v[k] = *reinterpret_cast<const u32x4 *>(x + pv * PER);
+    }
+    if constexpr (MODE == kUnevenHalves) {
+      *reinterpret_cast<u32x4 *>(&s_row[slot + SLOTS * k][pu * PER]) = u[k];
+      *reinterpret_cast<u32x4 *>(&s_row[slot + SLOTS * k][pv * PER]) = v[k];
     }
   }
   const int last = (count - 1 + first) / H;
@@ -116,9 +124,8 @@ template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bou
       u[k] = Piece<T>::pack(yu);
       v[k] = Piece<T>::pack(yv);
     }
-    if constexpr (NEIGHBOURS) {
-      auto turn = [&](u32x4 &w, int piece) {
-        if (piece >= turned) return;
+    if constexpr (MODE == kNeighbours) {
+      auto turn = [&](u32x4 &w, int piece) {   // words whose pairs are turned; the others stay
         float x[PER], z[PER];
         Piece<T>::unpack(w, x);
 #pragma unroll
@@ -127,7 +134,29 @@ template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bou
           z[2 * e] = x[2 * e] * co - x[2 * e + 1] * si;
           z[2 * e + 1] = x[2 * e] * si + x[2 * e + 1] * co;
         }
-        w = Piece<T>::pack(z);
+        const u32x4 y = Piece<T>::pack(z);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (PER * piece + PER / 4 * e) / 2 < a.half ? y[e] : w[e];
+      };
+      turn(u[k], pu);
+      turn(v[k], pv);
+    }
+    if constexpr (MODE == kUnevenHalves) {
+      const T *row = s_row[slot + SLOTS * k];
+      auto turn = [&](u32x4 &w, int piece) {
+        float x[PER], z[PER];
+        Piece<T>::unpack(w, x);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          const int ch = PER * piece + e;
+          const bool lower = ch < a.half, in = ch < 2 * a.half;
+          const int i = lower ? ch : in ? ch - a.half : 0;   // its pair
+          const float mate = to_f(row[lower ? ch + a.half : i]), si = cs[64 + i];
+          z[e] = x[e] * cs[i] + mate * (lower ? -si : si);
+        }
+        const u32x4 y = Piece<T>::pack(z);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = PER * piece + PER / 4 * e < 2 * a.half ? y[e] : w[e];
       };
       turn(u[k], pu);
       turn(v[k], pv);
@@ -139,32 +168,8 @@ template <typename T, bool NEIGHBOURS, bool STREAM> __global__ void __launch_bou
   }
 }
 
-// Pairs that do not fill whole pieces: one workgroup per token, a thread a pair of channels.
-template <typename T> __global__ void __launch_bounds__(256) k_rotary_pairs(Rotary a) {
-  const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  if (n >= a.N) return;
-  const int i = threadIdx.x % 64;   // a pair, or two channels behind the pairs
-  float c = 1.0f, s = 0.0f;
-  if (i < a.half) angle(a, n, turns_of(a, i), c, s);
-  const int u = i < a.half ? (a.neighbours ? 2 * i : i) : 2 * i, v = i < a.half && !a.neighbours ? i + a.half : u + 1;
-  for (int h = threadIdx.x / 64; h < a.heads[0] + a.heads[1]; h += 4) {
-    const int t = h >= a.heads[0], hh = h - (t ? a.heads[0] : 0);
-    const RotaryRows &r = a.r[t];
-    const T *x = (const T *)r.x + n * r.x_token + hh * r.x_head;
-    T *y = (T *)r.y + n * r.y_token + hh * r.y_head;
-    const T xu = x[u], xv = x[v];
-    y[u] = i < a.half ? (T)(to_f(xu) * c - to_f(xv) * s) : xu;
-    y[v] = i < a.half ? (T)(to_f(xu) * s + to_f(xv) * c) : xv;
-  }
-}
-
 template <typename T> static hipError_t launch_rotary_of(Rotary a, hipStream_t s) {
   const int H = a.heads[0] + a.heads[1];
-  if ((a.neighbours ? 2 * a.half : a.half) % kRotPer<T> != 0) {
-    const dim3 grid((unsigned)min(a.N, 65536), (unsigned)((a.N + 65535) / 65536));
-    hipLaunchKernelGGL(k_rotary_pairs<T>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
-  }
   a.by_heads = (65536 + H - 1) / H;   // used where H is below a workgroup's rows: exact for i < TILE + H
   auto go = [&](auto kern, int64_t tile) {
     const int64_t blocks = ((int64_t)a.N * H + tile - 1) / tile;
@@ -175,8 +180,9 @@ template <typename T> static hipError_t launch_rotary_of(Rotary a, hipStream_t s
   };
   const bool stream = (int64_t)a.N * H * kHeadDim * (int)sizeof(T) > kRotKept;
   if (a.neighbours)
-    return stream ? go(k_rotary<T, true, true>, kRotTile<T, true>) : go(k_rotary<T, true, false>, kRotTile<T, false>);
-  return stream ? go(k_rotary<T, false, true>, kRotTile<T, true>) : go(k_rotary<T, false, false>, kRotTile<T, false>);
+    return stream ? go(k_rotary<T, kNeighbours, true>, kRotTile<T, true>) : go(k_rotary<T, kNeighbours, false>, kRotTile<T, false>);
+  if (a.half % kRotPer<T> != 0) return go(k_rotary<T, kUnevenHalves, true>, kRotTile<T, true>);
+  return stream ? go(k_rotary<T, kHalves, true>, kRotTile<T, true>) : go(k_rotary<T, kHalves, false>, kRotTile<T, false>);
 }
 
 hipError_t launch_rotary(int dtype, const Rotary &a, hipStream_t s) {

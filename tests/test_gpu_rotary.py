@@ -166,15 +166,18 @@ def test_moves_compact_keys():
     assert (np.abs(np64(K) - want) <= 2 * 12 * U * 2 * np64(raw).max()).all()
 
 
-def test_non_finite_values_stay_in_their_pair():
-    freq = A().rotary_frequencies(64, 10000.0)
-    x = torch.ones(3, 2, 128, device="cuda")
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d_rot", [64, 34, 6])
+def test_non_finite_values_stay_in_their_pair(dtype, d_rot):
+    freq = A().rotary_frequencies(d_rot, 10000.0)
+    x = torch.ones(4, 2, 128, device="cuda", dtype=dtype)
     x[1, 0, 3] = math.nan
     x[2, 1, 100] = math.inf
-    for inter, mate in ((False, 35), (True, 2)):
-        y = A().rotary(x, freq, i32([5, 6, 7]), interleaved=inter)
+    x[3, 0, d_rot] = math.nan            # beside the last pair
+    for inter, mate in ((False, 3 + d_rot // 2 if d_rot > 6 else 0), (True, 2)):
+        y = A().rotary(x, freq, i32([5, 6, 7, 8]), interleaved=inter)
         bad = (~y.isfinite()).nonzero().tolist()
-        assert bad == sorted([[1, 0, 3], [1, 0, mate], [2, 1, 100]])
+        assert bad == sorted([[1, 0, 3], [1, 0, mate], [2, 1, 100], [3, 0, d_rot]])
 
 
 def test_many_tokens_and_heads():

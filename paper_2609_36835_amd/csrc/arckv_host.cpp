@@ -144,7 +144,7 @@ hipError_t launch_ncache_read(int dtype, const NCache &c, int first, int n, cons
 int attendn_chunks(int P, int rows, int F);
 hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const void *Kf, const void *Vf, const int32_t *length_f, float *part_o,
-                          float *part_ml, float *out, hipStream_t s);
+                          float *part_ml, float *out, int nch, hipStream_t s);
 hipError_t launch_rotary(int dtype, const Rotary &a, hipStream_t s);
 
 // ------------------------------------------------------------------ timing
@@ -1154,8 +1154,8 @@ static arckv_status check_attend_ncache(int32_t P, int32_t rows, int32_t G, int3
   return ARCKV_OK;
 }
 
-static size_t attend_ncache_ws_bytes(int32_t P, int32_t rows, int32_t G, int32_t F, size_t *ml) {
-  const size_t nch = (size_t)attendn_chunks(P, rows, F);
+// Bytes that partials of nch chunks a pair take; ml: where their maxima and sums begin.
+static size_t attend_ncache_ws_bytes(int32_t P, int32_t G, int nch, size_t *ml) {
   *ml = (size_t)rup((int64_t)((size_t)P * nch * G * kHeadDimH * 4), 256);
   return nch == 1 ? 0 : *ml + (size_t)rup((int64_t)((size_t)P * nch * G * 2 * 4), 256);
 }
@@ -1164,7 +1164,7 @@ arckv_status arckv_attend_ncache_workspace_size(int32_t P, int32_t rows, int32_t
   CHECK(check_attend_ncache(P, rows, G, F));
   if (!bytes) return ARCKV_ERR_INVALID_ARG;
   size_t ml;
-  *bytes = attend_ncache_ws_bytes(P, rows, G, F, &ml);
+  *bytes = attend_ncache_ws_bytes(P, G, attendn_chunks(P, rows, F), &ml);
   return ARCKV_OK;
 }
 
@@ -1178,12 +1178,13 @@ arckv_status arckv_attend_ncache(const arckv_ncache *c, int32_t G, int32_t F, fl
       !aligned(V_f, 16) || !aligned(length_f, 4) || !aligned(out, 16))
     return ARCKV_ERR_INVALID_ARG;
   size_t ml;
-  const size_t need = attend_ncache_ws_bytes(c->P, c->rows, G, F, &ml);
+  const int nch = attendn_chunks(c->P, c->rows, F);
+  const size_t need = attend_ncache_ws_bytes(c->P, G, nch, &ml);
   if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return ARCKV_ERR_WORKSPACE;
   const float s = scale > 0.0f ? scale : 1.0f / sqrtf((float)kHeadDimH);
   STAGE(ST_ATTEND_NCACHE,
         launch_attendn(make_ncache(c), G, F, s, Q, beta, length, F > 0 ? K_f : nullptr, F > 0 ? V_f : nullptr, length_f,
-                       (float *)ws, need ? (float *)((char *)ws + ml) : nullptr, out, stream));
+                       (float *)ws, need ? (float *)((char *)ws + ml) : nullptr, out, nch, stream));
   return ARCKV_OK;
 }
 

@@ -471,23 +471,26 @@ int attendn_chunks(int P, int rows, int F) {
   const int n = (units + kAnW - 1) / kAnW;
   int best = 1;
   int64_t least = INT64_MAX;
-  for (int c = 1; c <= n && (int64_t)P * (c - 1) < 2 * kAnSlots; ++c) {
+  // of the numbers that give a wave as many units the least is best
+  for (int c = 1; c <= n && (int64_t)P * (c - 1) < 2 * kAnSlots;) {
+    const int units_each = (n + c - 1) / c;
     const int64_t wgs = (int64_t)P * c, rounds = (wgs + kAnSlots - 1) / kAnSlots, on_cu = min((wgs + kCus - 1) / kCus, kAnSlots / kCus);
     const int64_t unit = wgs <= kCus / 2 ? kAlone : max(kLatency, kShare * on_cu);
-    const int64_t cost = rounds * ((n + c - 1) / c * unit + kStart + kMore * (on_cu - 1)) + (c > 1 ? kJoin + kJoinChunk * c : 0);
+    const int64_t cost = rounds * (units_each * unit + kStart + kMore * (on_cu - 1)) + (c > 1 ? kJoin + kJoinChunk * c : 0);
     if (cost < least) {
       least = cost;
       best = c;
     }
+    if (units_each == 1) break;
+    c = (n + units_each - 2) / (units_each - 1);
   }
   return best;
 }
 
 hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const void *Kf, const void *Vf, const int32_t *length_f, float *part_o,
-                          float *part_ml, float *out, hipStream_t s) {
-  AttendN a{c, G, F, scale, (const bf16 *)Q, beta, length, (const bf16 *)Kf, (const bf16 *)Vf, length_f, part_o, part_ml, out, 0};
-  a.nch = attendn_chunks(c.P, c.rows, F);
+                          float *part_ml, float *out, int nch, hipStream_t s) {
+  AttendN a{c, G, F, scale, (const bf16 *)Q, beta, length, (const bf16 *)Kf, (const bf16 *)Vf, length_f, part_o, part_ml, out, nch};
   // pairs over y and z: a grid's y extent is limited
   const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
   const bool stream = (int64_t)c.P * c.rows * 2 * kNRow > kAnKept;

@@ -157,7 +157,8 @@ __global__ void __launch_bounds__(256) k_ncache_read(NCache c, int first, int n,
   float s[kNrRows];
 #pragma unroll
   for (int k = 0; k < kNrRows; ++k) {
-    const int64_t at = max(min(first + i0 + k * STEP, len - 1), 0);   // in range always; rows past the end are not used
+    if (len == 0) break;   // nothing to read
+    const int64_t at = min(first + i0 + k * STEP, len - 1);   // rows past the end are not used
     if constexpr (PER == 8)
       w[k] = reinterpret_cast<const uint32_t *>(codes + at * kNRow)[piece];
     else

@@ -601,3 +601,88 @@ def test_compact_cache_in_4_bits():
     out = A().attend_ncache(Q, c, beta, None, K_f, V_f)
     m = [x.cpu().numpy() for x in c]
     check_attend(out, Q, c, beta, None, K_f, V_f, None)
+
+
+# ------------------------------------------------------------------------------------------------ large calls
+@pytest.mark.parametrize("dtype,n", [(torch.bfloat16, 30001), (torch.float32, 15003)])
+def test_large_write_is_many_small_ones(dtype, n):
+    """A write whose source is read as a stream leaves the same bytes as one in pieces."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    P = 8
+    K, V = (torch.randn(P, n, 128, device="cuda", generator=g).to(dtype) for _ in range(2))
+    whole, pieces = make_cache(P, n + 5), make_cache(P, n + 5)
+    A().ncache_write(whole, K, V, i32([3] * P))
+    for a in range(0, n, 4000):
+        b = min(a + 4000, n)
+        A().ncache_write(pieces, K[:, a:b].contiguous(), V[:, a:b].contiguous(), i32([3 + a] * P))
+    assert all(torch.equal(a, b) for a, b in zip(whole, pieces))
+
+
+@pytest.mark.parametrize("G", [4, 8, 16])
+def test_large_attend(G):
+    """A call whose codes are read as streams, with bias, lengths and tail: some of its pairs against the oracle, all of them
+    against calls of few pairs (other chunks, other order of sums)."""
+    g = np.random.default_rng(G)
+    P, R, F = 300, 3001, 40
+    c = make_cache(P, R)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(G)
+    randn = lambda *s: torch.randn(*s, device="cuda", generator=gen)
+    length = g.integers(1, R + 1, P).tolist()
+    A().ncache_write(c, randn(P, R, 128).bfloat16(), randn(P, R, 128).bfloat16(), None, i32(length))
+    Q, K_f, V_f = randn(P, G, 128).bfloat16(), randn(P, F, 128).bfloat16(), randn(P, F, 128).bfloat16()
+    beta = randn(P, R)
+    beta[:, ::5] = -math.inf
+    print(f"large attend G={G}", flush=True)
+    out = A().attend_ncache(Q, c, beta, i32(length), K_f, V_f)
+    for p in (0, 17, 150, 299):
+        check_attend(out[p:p + 1], Q[p:p + 1], [t[p:p + 1] for t in c], beta[p:p + 1], length[p:p + 1], K_f[p:p + 1], V_f[p:p + 1], None)
+    for a in range(0, P, 25):
+        part = slice(a, a + 25)
+        few = A().attend_ncache(Q[part].contiguous(), tuple(t[part].contiguous() for t in c), beta[part].contiguous(), i32(length[part]),
+                                K_f[part].contiguous(), V_f[part].contiguous())
+        # each is within check_attend's bound of the formula: here 2 (2^-17 + 6 * 3041 * 2^-24) of a mean |v| below 1
+        assert (few - out[part]).abs().max() <= 4 * (2.0 ** -17 + 6 * 3041 * U)
+
+
+def test_many_pairs():
+    """Pairs beyond one extent of a grid."""
+    g = np.random.default_rng(22)
+    P, R, G = 70000, 3, 1
+    K, V, Q = (torch.randn(P, n, 128, device="cuda").bfloat16() for n in (R, R, G))
+    c = make_cache(P, R)
+    A().ncache_write(c, K, V)
+    k, v = A().ncache_read(c, 1, 2)
+    print("many pairs", flush=True)
+    out = A().attend_ncache(Q, c, None, i32([2] * P))
+    for p in (0, 1, 32767, 32768, 32769, 65535, 65536, P - 1):
+        m = [t[p:p + 1] for t in c]
+        same(m, [x[None] for x in (*(on.n_bytes(*on.n_rows(np64(K[p])))[:1]), on.n_bytes(*on.n_rows(np64(V[p])))[0],
+                                   on.n_bytes(*on.n_rows(np64(K[p])))[1], on.n_bytes(*on.n_rows(np64(V[p])))[1])])
+        assert np.array_equal(np64(k[p]), on.n_values(*on.n_rows(np64(K[p])))[1:])
+        assert np.array_equal(np64(v[p]), on.n_values(*on.n_rows(np64(V[p])))[1:])
+        check_attend(out[p:p + 1], Q[p:p + 1], m, None, [2], None, None, None)
+
+
+@pytest.mark.parametrize("G", [2, 8, 16])
+def test_attend_infinite_tail_values(G):
+    """An infinite value of the tail makes its channel infinite, and nothing else."""
+    g = np.random.default_rng(23)
+    c = filled(g, 2, 200)
+    Q, K_f, V_f = rows(g, 2, G, 128), rows(g, 2, 40, 128), rows(g, 2, 40, 128)
+    V_f[0, 35, 7] = math.inf
+    V_f[0, 3, 100] = -math.inf
+    out = A().attend_ncache(Q, c, None, None, K_f, V_f)
+    assert (out[0, :, 7] == math.inf).all() and (out[0, :, 100] == -math.inf).all()
+    out[0, :, 7] = out[0, :, 100] = 0
+    assert out.isfinite().all()
+
+
+def test_binding_refuses_what_32_bits_do_not_hold():
+    c = A().ncache(2, 50)
+    for big in (1 << 31, 1 << 32, -(1 << 31) - 1):
+        with pytest.raises(ValueError, match="first"):
+            A().ncache_read(c, big, 4)
+        with pytest.raises(ValueError, match="n:"):
+            A().ncache_read(c, 0, big)

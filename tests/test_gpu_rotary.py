@@ -236,3 +236,34 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         check(y, q, p, freq, transpose=True)
         check(z, k, p, freq, transpose=True)
+
+
+@pytest.mark.parametrize("dtype,N", [(torch.bfloat16, 2300), (torch.float32, 1150)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d_rot", [128, 64, 34])
+def test_large_calls(dtype, N, interleaved, d_rot):
+    """Rows that are read as streams (over 64 MiB), 101 + 20 heads: some tokens against the oracle, all of them against calls of
+    few tokens."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d_rot)
+    x = torch.randn(N, 121, 128, device="cuda", generator=g).to(dtype)
+    freq = A().rotary_frequencies(d_rot, 10000.0)
+    pos = torch.randint(0, 100000, (N,), device="cuda", generator=g).int()
+    y, z = A().rotary(x[:, :101], freq, pos, x[:, 101:], interleaved=interleaved)
+    for n in (0, 1, N // 2, N - 1):
+        check(y[n:n + 1], x[n:n + 1, :101], pos[n:n + 1].tolist(), freq, interleaved)
+        check(z[n:n + 1], x[n:n + 1, 101:], pos[n:n + 1].tolist(), freq, interleaved)
+    for a in range(0, N, 230):
+        few = A().rotary(x[a:a + 230], freq, pos[a:a + 230].contiguous(), interleaved=interleaved)
+        assert torch.equal(few[:, :101], y[a:a + 230]) and torch.equal(few[:, 101:], z[a:a + 230])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("heads", [15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200])
+def test_heads_around_a_workgroups_rows(dtype, interleaved, heads):
+    g = np.random.default_rng(heads)
+    for d_rot in (128, 34):
+        freq, pos = A().rotary_frequencies(d_rot, 10000.0), g.integers(0, 5000, 5)
+        x = rows(g, 5, heads, 128, dtype=dtype)
+        check(A().rotary(x, freq, i32(pos), interleaved=interleaved), x, pos, freq, interleaved)

@@ -231,7 +231,10 @@ def filled(g, P, R, kscale=1.0):
 
 SIZES = [(1, 1, 1, 0), (2, 1, 4, 1), (3, 63, 1, 0), (2, 64, 2, 31), (5, 65, 3, 32), (2, 128, 4, 33), (3, 200, 5, 7),
          (2, 1000, 8, 64), (2, 1025, 9, 0), (1, 4097, 16, 300), (8, 819, 4, 37), (1, 20000, 7, 0), (40, 130, 12, 1),
-         (300, 700, 4, 40), (2, 33000, 4, 0), (800, 70, 1, 3)]
+         (300, 700, 4, 40), (2, 33000, 4, 0), (800, 70, 1, 3),
+         # about a workgroup's width: five blocks are one more than four waves take at once, 257 pairs one more than there are CUs
+         (3, 256, 3, 0), (3, 257, 6, 0), (4, 256, 16, 1), (7, 512, 2, 33), (4, 513, 12, 64), (6, 1, 4, 190), (256, 330, 3, 0),
+         (257, 330, 3, 0), (200, 2700, 4, 0), (200, 2700, 10, 1)]
 
 
 @pytest.mark.parametrize("P,R,G,F", SIZES)

@@ -9,9 +9,9 @@ def test_a_waves_exchanges_are_fenced_on_both_sides(tmp_path):
     """Scales and biases, and the terms of probabilities, go through LDS to other lanes in every turn of the loop over
     blocks: stores, a fence, loads, and a fence again before the next turn's stores."""
     found = {n: b for n, b in kernels_ir("attend_n.hip", tmp_path).items() if "k_attendn_partial" in n}
-    assert len(found) == 12
+    assert len(found) == 24
     for name, blocks in found.items():
-        queries = int(re.search(r"ILi(\d+)E", name)[1])
+        queries = int(re.search(r"ILi\d+ELi(\d+)E", name)[1])
         scales = [s for s in (exchanges(b, r"(?:i32|float|i8|<4 x float>)") for b in blocks) if re.search("w.*r", s)]
         assert len(scales) == 1 and re.fullmatch("f?r?w+fr+", scales[0].replace("ff", "f")), (name, scales)
         terms = [s for s in (exchanges(b, r"(?:<2 x i32>|<8 x bfloat>)") for b in blocks) if re.search("w.*r", s)]

@@ -1,12 +1,14 @@
 // Rotary positions: pairs of channels turned by position * frequency.
 //
 // HBM-bound: every row is read and written once.  A row is cut into pieces of 16 bytes, and a thread takes the two that
-// belong together (channels c .. and c + half .., or neighbours) of one row or four, all loaded before the angles are
+// belong together (channels c .. and c + half .., or neighbours) of one row or two, all loaded before the angles are
 // formed: a workgroup's rows follow each other through tokens and heads, so it needs the angles of few tokens, each formed
 // once, by one thread, for all its heads, and handed out through LDS.  Halves that end inside a piece have their rows in LDS
 // too, where a channel finds its mate at any distance.
 // 32768 tokens of 40 bf16 heads, out of a fused projection, take 113 us (5.9 TB/s), 4093 of 20 float32 heads 13.5 (6.2); a thread
 // a pair of channels took 274 and 22.9.  16384 of 40 heads with 34 channels turned take 71 us in halves, 60 as neighbours.
+#include <type_traits>
+
 #include "common.hpp"
 #include "qcode.hpp"
 #include "rotary.hpp"
@@ -15,13 +17,18 @@ namespace arckv {
 
 namespace {
 constexpr int kRotThreads = 256;
-// Bytes above which rows are read as streams that the caches do not keep: 4096 tokens of 40 heads (42 MB in) take 14.1 us kept
-// and 14.8 streamed, 32768 tokens (336 MB) 125.5 and 122.8, 262144 of two heads (134 MB) 63.5 and 59.5.
-constexpr int64_t kRotKept = (int64_t)64 << 20;
-template <bool STREAM> constexpr int kRotRows = STREAM ? 1 : 4;   // of a thread: 113.0 and 123.1 us streamed, 16.1 and 14.1 kept
+// Bytes above which rows are read as streams that the caches do not keep.  us kept and streamed: 4096 tokens of 40 bf16 heads (42
+// MB in) 13.9 and 16.3, 8000 (82 MB) 25.5 and 29.6, 9500 (97 MB) 33.5 and 34.6, 12000 (123 MB) 42.8 and 40.9, 32768 (336 MB) 114
+// and 107.
+constexpr int64_t kRotKept = (int64_t)96 << 20;
+// Bytes above which, if not streamed, a thread takes two rows instead of one, where tokens have more than one head (one head's rows
+// need as many angles as there are channels).  us with one, two and four: 64 tokens of 40 bf16 heads 2.8, 3.2, 3.9; 1000 (10 MB)
+// 4.9, 5.0, 5.7; 2000 (20 MB) 8.3, 7.8, 7.9; 4096 (42 MB) 15.7, 13.9, 13.2; 4093 of 20 float32 heads (42 MB) 15.1, 13.7, 13.4;
+// 65536 of 5 (84 MB) 30.9, 27.2, 27.5; 131072 of one (34 MB) 18.4, 20.6, 25.8; 32768 of 40, streamed, 113.0 with one, 123.1 with four.
+constexpr int64_t kRotFew = (int64_t)16 << 20;
 template <typename T> constexpr int kRotPer = 16 / (int)sizeof(T);                     // channels of a piece
 template <typename T> constexpr int kRotSlots = kRotThreads * 2 * kRotPer<T> / kHeadDim;  // rows that threads take at a time
-template <typename T, bool STREAM> constexpr int kRotTile = kRotSlots<T> * kRotRows<STREAM>;   // and a workgroup in all
+template <typename T, int ROWS> constexpr int kRotTile = kRotSlots<T> * ROWS;             // and a workgroup in all
 
 // Turns per position of a pair.
 __device__ inline double turns_of(const Rotary &a, int i) { return a.freq[i] * 0.15915494309189533577; }
@@ -61,8 +68,8 @@ template <> struct Piece<bf16> {
 
 enum RotaryMode { kHalves, kNeighbours, kUnevenHalves };
 
-template <typename T, int MODE, bool STREAM> __global__ void __launch_bounds__(kRotThreads) k_rotary(Rotary a) {
-  constexpr int PER = kRotPer<T>, THREADS = kHeadDim / (2 * PER), SLOTS = kRotSlots<T>, ROWS = kRotRows<STREAM>, TILE = kRotTile<T, STREAM>;
+template <typename T, int MODE, int ROWS, bool STREAM> __global__ void __launch_bounds__(kRotThreads) k_rotary(Rotary a) {
+  constexpr int PER = kRotPer<T>, THREADS = kHeadDim / (2 * PER), SLOTS = kRotSlots<T>, TILE = kRotTile<T, ROWS>;
   extern __shared__ __align__(16) float s_angle[];   // [token][cos, sin][64]
   __shared__ __align__(16) T s_row[MODE == kUnevenHalves ? TILE : 1][kHeadDim];
   const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
@@ -173,6 +180,7 @@ template <typename T, int MODE, bool STREAM> __global__ void __launch_bounds__(k
 template <typename T> static hipError_t launch_rotary_of(Rotary a, hipStream_t s) {
   const int H = a.heads[0] + a.heads[1];
   a.by_heads = (65536 + H - 1) / H;   // used where H is below a workgroup's rows: exact for i < TILE + H
+  const int64_t bytes = (int64_t)a.N * H * kHeadDim * (int)sizeof(T);
   auto go = [&](auto kern, int64_t tile) {
     const int64_t blocks = ((int64_t)a.N * H + tile - 1) / tile;
     const dim3 grid((unsigned)min(blocks, (int64_t)65536), (unsigned)((blocks + 65535) / 65536));
@@ -180,11 +188,15 @@ template <typename T> static hipError_t launch_rotary_of(Rotary a, hipStream_t s
     hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), tokens * 128 * sizeof(float), s, a);
     return hipGetLastError();
   };
-  const bool stream = (int64_t)a.N * H * kHeadDim * (int)sizeof(T) > kRotKept;
-  if (a.neighbours)
-    return stream ? go(k_rotary<T, kNeighbours, true>, kRotTile<T, true>) : go(k_rotary<T, kNeighbours, false>, kRotTile<T, false>);
-  if (a.half % kRotPer<T> != 0) return go(k_rotary<T, kUnevenHalves, true>, kRotTile<T, true>);
-  return stream ? go(k_rotary<T, kHalves, true>, kRotTile<T, true>) : go(k_rotary<T, kHalves, false>, kRotTile<T, false>);
+  auto by_rows = [&](auto mode) {
+    constexpr int MODE = decltype(mode)::value;
+    if (bytes > kRotKept) return go(k_rotary<T, MODE, 1, true>, kRotTile<T, 1>);
+    if constexpr (MODE != kUnevenHalves)
+      if (bytes > kRotFew && H > 1) return go(k_rotary<T, MODE, 2, false>, kRotTile<T, 2>);
+    return go(k_rotary<T, MODE, 1, false>, kRotTile<T, 1>);
+  };
+  if (a.neighbours) return by_rows(std::integral_constant<int, kNeighbours>{});
+  return a.half % kRotPer<T> == 0 ? by_rows(std::integral_constant<int, kHalves>{}) : by_rows(std::integral_constant<int, kUnevenHalves>{});
 }
 
 hipError_t launch_rotary(int dtype, const Rotary &a, hipStream_t s) {

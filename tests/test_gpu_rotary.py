@@ -238,11 +238,11 @@ def test_streams_and_graphs():
         check(z, k, p, freq, transpose=True)
 
 
-@pytest.mark.parametrize("dtype,N", [(torch.bfloat16, 2300), (torch.float32, 1150)])
+@pytest.mark.parametrize("dtype,N", [(torch.bfloat16, 3300), (torch.float32, 1650)])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("d_rot", [128, 64, 34])
 def test_large_calls(dtype, N, interleaved, d_rot):
-    """Rows that are read as streams (over 64 MiB), 101 + 20 heads: some tokens against the oracle, all of them against calls of
+    """Rows that are read as streams (over 96 MiB), 101 + 20 heads: some tokens against the oracle, all of them against calls of
     few tokens."""
     g = torch.Generator(device="cuda")
     g.manual_seed(d_rot)
@@ -260,10 +260,42 @@ def test_large_calls(dtype, N, interleaved, d_rot):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("N,heads", [(70001, 1), (40001, 2), (30001, 3), (2901, 31), (2701, 33), (1301, 63), (1300, 64), (1299, 65), (700, 121)])
+def test_middle_calls(dtype, N, heads, interleaved):
+    """Rows of 16 to 96 MiB: some tokens against the oracle, all of them against calls of fewer bytes."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(heads)
+    x = torch.randn(N, heads, 128, device="cuda", generator=g).to(dtype)
+    pos = torch.randint(0, 100000, (N,), device="cuda", generator=g).int()
+    for d_rot in (128, 34):
+        freq = A().rotary_frequencies(d_rot, 10000.0)
+        y = A().rotary(x, freq, pos, interleaved=interleaved)
+        for n in (0, 1, N // 2, N - 1):
+            check(y[n:n + 1], x[n:n + 1], pos[n:n + 1].tolist(), freq, interleaved)
+        step = N // 7 + 1
+        for a in range(0, N, step):
+            few = A().rotary(x[a:a + step], freq, pos[a:a + step].contiguous(), interleaved=interleaved)
+            assert torch.equal(few, y[a:a + step])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("heads", [15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200])
 def test_heads_around_a_workgroups_rows(dtype, interleaved, heads):
     g = np.random.default_rng(heads)
     for d_rot in (128, 34):
         freq, pos = A().rotary_frequencies(d_rot, 10000.0), g.integers(0, 5000, 5)
         x = rows(g, 5, heads, 128, dtype=dtype)
+        check(A().rotary(x, freq, i32(pos), interleaved=interleaved), x, pos, freq, interleaved)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("N,heads", [(127, 1), (128, 1), (129, 1), (1000, 1), (400, 2), (300, 3)])
+def test_few_heads(dtype, interleaved, N, heads):
+    """Workgroups whose rows are of as many tokens as rows, or nearly: the most angles that one forms."""
+    g = np.random.default_rng(N)
+    for d_rot in (128, 34):
+        freq, pos = A().rotary_frequencies(d_rot, 10000.0), g.integers(0, 100000, N)
+        x = rows(g, N, heads, 128, dtype=dtype)
         check(A().rotary(x, freq, i32(pos), interleaved=interleaved), x, pos, freq, interleaved)

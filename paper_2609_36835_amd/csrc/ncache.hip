@@ -14,13 +14,16 @@ constexpr int kGridY = 32768;
 
 // ---------------------------------------------------------------- write
 // HBM-bound: 2 (or 4) bytes in and 17 / 32 out per element, once.  Sixteen lanes take a row, 16 bytes of whole lines at a
-// time, a thread four rows (bf16) or one (float32), and a wave consecutive rows, whose scales go out as one piece.  Codes are
-// written as streams.  64 pairs of 1024 to 2048 bf16 rows take 12.3 us, 256 of 3277 float32 rows 150 us (6.5 TB/s; 193 with a
-// group per thread, 179 with four rows and half lines per load, 164 kept in the caches).
-template <typename T> constexpr int kNwRows = sizeof(T) == 2 ? 4 : 1;   // of a thread
-template <typename T> constexpr int kNwTile = 4 * 4 * kNwRows<T>;       // of a workgroup of four waves
+// time, a thread one row of float32 and up to four of bf16, and a wave consecutive rows, whose scales go out as one piece.
+// Codes are written as streams.  64 pairs of 1024 to 2048 bf16 rows take 12.3 us, 256 of 3277 float32 rows 150 us (6.5 TB/s;
+// 193 with a group per thread, 179 with four rows and half lines per load, 164 kept in the caches).
+template <int ROWS> constexpr int kNwTile = 4 * 4 * ROWS;   // rows of a workgroup of four waves, ROWS to a thread
+// Source bytes of bf16 up to which a thread takes one row.  us with one, two and four: 512 pairs of one row 2.5, 2.9, 3.1; 8 of
+// 2048 (8 MB) 3.3, 3.3, 3.5; 64 of 500 (16 MB) 4.6, 4.4, 4.7; of 2048 (67 MB) 14.8, 13.7, 12.8.
+constexpr int64_t kNwFew = (int64_t)16 << 20;
 // Source bytes above which rows are read as streams that the caches do not keep: 64 pairs of 2048 bf16 rows (67 MB) take 14.7 us
-// kept and 15.7 streamed, of 4096 30.7 and 28.7.
+// kept and 15.7 streamed, of 4096 30.7 and 28.7.  Streams of bf16 take two rows a thread: with two and with four 256 pairs of
+// 2048 54.2 and 55.1, 8 of 131072 104.8 and 109.7, 512 of 3277 170 and 185.
 constexpr int64_t kNwKept = (int64_t)96 << 20;
 
 // The largest of four lanes' values, in all of them; of eight.
@@ -85,17 +88,17 @@ __device__ inline uint32_t encode(const u32x4 (&w)[2], int r, int &at, uint32_t 
   return r & 1 ? other | code[1] << 16 : code[0] | other << 16;
 }
 
-template <typename T, bool STREAM>
+template <typename T, int ROWS, bool STREAM>
 __global__ void __launch_bounds__(256) k_ncache_write(NCache c, int n, const T *__restrict__ K, const T *__restrict__ V,
                                                       const int32_t *__restrict__ starts,
                                                       const int32_t *__restrict__ counts) {
-  constexpr int LOADS = sizeof(T) / 2, ROWS = kNwRows<T>;
+  constexpr int LOADS = sizeof(T) / 2;
   const int p = (blockIdx.z >> 1) * gridDim.y + blockIdx.y;
   if (p >= c.P) return;
   const int start = clip_len(starts, p, starts ? c.rows : 0);
   const int count = min(clip_len(counts, p, n), c.rows - start);
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  const int i0 = blockIdx.x * kNwTile<T> + (threadIdx.x >> 6) * 4 * ROWS;   // the wave's rows i0 + 4 k + g
+  const int i0 = blockIdx.x * kNwTile<ROWS> + (threadIdx.x >> 6) * 4 * ROWS;   // the wave's rows i0 + 4 k + g
   if (i0 >= count) return;
   const T *src = (blockIdx.z & 1 ? V : K) + ((int64_t)p * n + i0) * kHeadDim;
   const int64_t row0 = (int64_t)p * c.rows + start + i0;
@@ -123,18 +126,24 @@ __global__ void __launch_bounds__(256) k_ncache_write(NCache c, int n, const T *
 
 hipError_t launch_ncache_write(int dtype, const NCache &c, int n, const void *K, const void *V, const int32_t *start,
                                const int32_t *count, hipStream_t s) {
-  auto go = [&](auto kern, auto *k, auto *v) {
-    const int tile = kNwTile<std::remove_const_t<std::remove_pointer_t<decltype(k)>>>;
+  auto go = [&](auto kern, auto rows, auto *k, auto *v) {
+    const int tile = kNwTile<decltype(rows)::value>;
     const dim3 grid((unsigned)((n + tile - 1) / tile), (unsigned)min(c.P, kGridY), (unsigned)(2 * ((c.P + kGridY - 1) / kGridY)));
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, c, n, k, v, start, count);
     return hipGetLastError();
   };
-  const bool stream = (int64_t)c.P * n * 2 * kHeadDim * (dtype == ARCKV_BF16 ? 2 : 4) > kNwKept;
-  if (dtype == ARCKV_BF16)
-    return stream ? go(k_ncache_write<bf16, true>, (const bf16 *)K, (const bf16 *)V)
-                  : go(k_ncache_write<bf16, false>, (const bf16 *)K, (const bf16 *)V);
-  return stream ? go(k_ncache_write<float, true>, (const float *)K, (const float *)V)
-                : go(k_ncache_write<float, false>, (const float *)K, (const float *)V);
+  constexpr std::integral_constant<int, 1> one{};
+  constexpr std::integral_constant<int, 2> two{};
+  constexpr std::integral_constant<int, 4> four{};
+  const int64_t bytes = (int64_t)c.P * n * 2 * kHeadDim * (dtype == ARCKV_BF16 ? 2 : 4);
+  if (dtype == ARCKV_BF16) {
+    const bf16 *k = (const bf16 *)K, *v = (const bf16 *)V;
+    return bytes <= kNwFew    ? go(k_ncache_write<bf16, 1, false>, one, k, v)
+           : bytes <= kNwKept ? go(k_ncache_write<bf16, 4, false>, four, k, v)
+                              : go(k_ncache_write<bf16, 2, true>, two, k, v);
+  }
+  return bytes <= kNwKept ? go(k_ncache_write<float, 1, false>, one, (const float *)K, (const float *)V)
+                          : go(k_ncache_write<float, 1, true>, one, (const float *)K, (const float *)V);
 }
 
 // ---------------------------------------------------------------- read

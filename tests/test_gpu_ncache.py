@@ -622,6 +622,32 @@ def test_large_write_is_many_small_ones(dtype, n):
     assert all(torch.equal(a, b) for a, b in zip(whole, pieces))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [450, 701, 1801])
+def test_larger_ragged_writes(dtype, n):
+    """Writes of 15 to 236 MB with a start and a count for each pair leave the same bytes as writes of a few pairs, and the others
+    as they were."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    P, R = 64, 2000
+    K, V = (torch.randn(P, n, 128, device="cuda", generator=g).to(dtype) for _ in range(2))
+    start = torch.randint(0, R - 100, (P,), device="cuda", generator=g).int()
+    count = torch.randint(0, n + 1, (P,), device="cuda", generator=g).int()
+    count[:8] = i32([0, 1, 15, 16, 17, n, n + 3, -1])
+    start[8:12] = i32([R - 1, R - 5, R, 0])
+    whole, few = make_cache(P, R), make_cache(P, R)
+    for t in (*whole, *few):
+        t.fill_(0xab)
+    A().ncache_write(whole, K, V, start, count)
+    for a in range(0, P, 4):
+        part = [t[a:a + 4] for t in few]
+        A().ncache_write(tuple(part), K[a:a + 4], V[a:a + 4], start[a:a + 4].contiguous(), count[a:a + 4].contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(whole, few))
+    for p in (0, 5, 9, 40):
+        b = max(0, min(int(count[p]), n, R - int(start[p]))) + int(start[p])
+        assert all((t[p, b:] == 0xab).all() and (t[p, :int(start[p])] == 0xab).all() for t in whole)
+
+
 @pytest.mark.parametrize("G", [4, 8, 16])
 def test_large_attend(G):
     """A call whose codes are read as streams, with bias, lengths and tail: some of its pairs against the oracle, all of them

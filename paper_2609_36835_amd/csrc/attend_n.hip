@@ -120,8 +120,13 @@ __device__ inline void make_queries(const AttendN &a, int p, const QueryWords<W,
   if (a.F > 0)
     for (int i = threadIdx.x; i < 4 * 64; i += 64 * W) {
       const int ks = i / 64, lane = i % 64, g = lane >> 4, r = lane & 15;
-      s.tail[i] = *reinterpret_cast<const bf16x8 *>(a.Q + ((int64_t)p * a.G + min(r % GP, a.G - 1)) * kHeadDim + 64 * (ks / 2) +
-                                                    16 * g + 8 * (ks % 2));
+      u32x4 w = *reinterpret_cast<const u32x4 *>(a.Q + ((int64_t)p * a.G + min(r % GP, a.G - 1)) * kHeadDim + 64 * (ks / 2) +
+                                                 16 * g + 8 * (ks % 2));
+      // An infinite channel enters as NaN, as it does over the blocks: its logits could all be -inf, which marks rows left out.
+      // Adding 0x80 carries into a half's top bit from the largest exponent alone.
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] |= (((w[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 9;
+      s.tail[i] = __builtin_bit_cast(bf16x8, w);
     }
 }
 

@@ -537,6 +537,9 @@ arckv_status arckv_ncache_read(const arckv_ncache *c, int32_t first, int32_t n, 
  *   length_f [P] device array of rows held in K_f, V_f (clipped to [0, F]), or NULL: F.
  *   out      [P][G][128] float32; zeros for a pair without any row to attend to, NaN
  *            for a query row with a non-finite channel where there is one.
+ * A mean of finite values is finite, however large they are and however many; for it sums
+ * are held in units in which up to (rows + F)^2 2^-114 of a result may be lost, whatever
+ * its size.  A logit of -inf in float32 counts as a row left out.
  * Tensors 16-byte aligned (per-pair int32 and float32 arrays by element).  Workspace:
  * arckv_attend_ncache_workspace_size bytes; 0 where a pair's rows are one
  * workgroup's work, ws may then be NULL.  Reads every code once. */

@@ -23,7 +23,10 @@
 //
 // Values become bf16, scale included, in registers (exact); probabilities enter (P V)^T as three bf16 terms that sum to
 // them exactly, as columns beside the queries again where there is room.  The columns of both products are the same queries,
-// so a query's sums sit with its running maximum.
+// so a query's sums sit with its running maximum.  P V is held times 2^-S, 2^S > 2 (rows + F): probabilities are at most 1, so
+// sums over the largest values stay below float32's end, and a mean that is finite comes out so.  A power of two costs no
+// bit where nothing falls below 2^-126; the scales of a block's values take it, a tail's probabilities, and once the sum of
+// probabilities that divides.
 #include <type_traits>
 
 #include "attend_parts.hpp"
@@ -38,9 +41,8 @@ constexpr int kAnMore = 8;            // of one that has a whole pair, and a CU,
 constexpr int kAnCus = 256;
 constexpr int kAnSlots = 3 * kAnCus;  // workgroups that run at a time
 constexpr int kAnPlanes = 4;
-// How far the reference of the exponentials is set above the largest logit when one passes it: probabilities stay below 1 (so
-// that large values do not overflow beside them) and the largest above 2^-8 or so, and sums are rescaled a few times in a call
-// instead of at every block.
+// How far the reference of the exponentials is set above the largest logit when one passes it: the largest probability stays
+// between 2^-8 or so and 1, and sums are rescaled a few times in a call instead of at every block.
 constexpr float kAnLead = 5.5451774f;
 // Bytes above which codes are read as streams that the caches do not keep: 64 pairs of 8192 rows (71 MB) take 18.2 us kept and
 // 19.2 streamed, of 12000 24.8 and 24.5, of 16384 31.7 and 29.2, three caches in turn.
@@ -60,6 +62,7 @@ struct AttendN {
   const int32_t *length_f;
   float *part_o, *part_ml, *out;
   int nch;                    // chunks per pair
+  float down;                 // 2^-S
 };
 
 namespace {
@@ -232,10 +235,10 @@ __device__ inline void attend_blocks(const AttendN &a, int p, int first, int end
       // zero times NaN is not zero: a row left out is finite.  (255, a NaN's byte, becomes an infinity, which converts to NaN.)
       const uint32_t vs = BETA && d.bias == -INFINITY ? 0x7f7f7f7fu : d.vs;
       s.ks[place] = d.ks;
-      s.vs[0][place] = __uint_as_float((vs & 255u) << 23);
-      s.vs[1][place] = __uint_as_float((vs >> 8 & 255u) << 23);
-      s.vs[2][place] = __uint_as_float((vs >> 16 & 255u) << 23);
-      s.vs[3][place] = __uint_as_float(vs >> 24 << 23);
+      s.vs[0][place] = __uint_as_float((vs & 255u) << 23) * a.down;
+      s.vs[1][place] = __uint_as_float((vs >> 8 & 255u) << 23) * a.down;
+      s.vs[2][place] = __uint_as_float((vs >> 16 & 255u) << 23) * a.down;
+      s.vs[3][place] = __uint_as_float(vs >> 24 << 23) * a.down;
       if constexpr (BETA) s.bias[place] = lane < live ? d.bias : -INFINITY;
     }
     wave_exchange();
@@ -412,7 +415,7 @@ __global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 2) k_attendn_partial(A
   if (end > blocks) {
     const int skip = first < blocks ? (blocks - first + W - 1) / W * W : 0;   // this wave's blocks
     const int tfirst = first + skip - blocks, tend = end - blocks;
-    if (tfirst < tend) attend_tail<W, false, STREAM, GP>(a, p, tfirst, tend, len_f, sQ.tail, m, l, o);
+    if (tfirst < tend) attend_tail<W, false, STREAM, GP>(a, p, tfirst, tend, len_f, sQ.tail, m, l, o, a.down);
   }
   // the terms' sums meet
   if constexpr (C > 1)
@@ -425,7 +428,7 @@ __global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 2) k_attendn_partial(A
       }
   if (g == 0 && r < G) {
     sM[wave][r] = m;
-    sL[wave][r] = l;
+    sL[wave][r] = l * a.down;   // as the sums beside it are
   }
   wave_exchange();
   if (r < G)
@@ -500,7 +503,8 @@ int attendn_chunks(int P, int rows, int F) {
 hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void *Q, const float *beta,
                           const int32_t *length, const void *Kf, const void *Vf, const int32_t *length_f, float *part_o,
                           float *part_ml, float *out, int nch, hipStream_t s) {
-  AttendN a{c, G, F, scale, (const bf16 *)Q, beta, length, (const bf16 *)Kf, (const bf16 *)Vf, length_f, part_o, part_ml, out, nch};
+  AttendN a{c, G, F, scale, (const bf16 *)Q, beta, length, (const bf16 *)Kf, (const bf16 *)Vf, length_f, part_o, part_ml, out, nch,
+            ldexpf(1.0f, -2 - (63 - __builtin_clzll((int64_t)c.rows + F)))};
   // pairs over y and z: a grid's y extent is limited
   const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
   const bool stream = (int64_t)c.P * c.rows * 2 * kNRow > kAnKept;

@@ -120,10 +120,11 @@ __device__ inline void load_tail_values(const A &a, int64_t row0, int live, u32x
 }
 
 // The tail's units of 32 rows first, first + W, ... below end, a wave's share of a chunk (ONE: one at most).  The queries
-// stand in the first COLS of the 16 columns; sums in the others, whose maximum goes along, only keep up with it.
+// stand in the first COLS of the 16 columns; sums in the others, whose maximum goes along, only keep up with it.  Probabilities
+// enter the product, not their sum, times `down`.
 template <int W, bool ONE, bool STREAM, int COLS, typename A>
 __device__ inline void attend_tail(const A &a, int p, int first, int end, int len, const bf16x8 *s_q, float &m,
-                                   float &l, f32x4 (&o)[8]) {
+                                   float &l, f32x4 (&o)[8], float down = 1.0f) {
   constexpr int NTV = STREAM ? kStreamed : 0;
   const int lane = threadIdx.x & 63, g = lane >> 4;
   const int64_t pr = (int64_t)p * a.F;
@@ -150,6 +151,8 @@ __device__ inline void attend_tail(const A &a, int p, int first, int end, int le
     bool any;
     float now;
     const float keep = softmax_step<8, 1, 0, false>(sv, m, l, any, now);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sv[i] *= down;
     Frag ph, pm, pl;
     split_p(sv, ph, pm, pl);
 #pragma unroll

@@ -802,6 +802,8 @@ def rotary(x, freq, positions=None, other=None, interleaved: bool = False, trans
     transpose, its gradient's way back.  `other` are rows of the same tokens (a layer's keys beside its queries), turned
     by the same call.  Strides of tokens and heads are free; out and out_other may be given (the inputs themselves, or
     tensors that share no row with them).  Returns out, or (out, out_other)."""
+    if other is None and out_other is not None:
+        raise ValueError("out_other: there are no rows (other) to turn into it")
     dev, dtype = torch.cuda.current_device(), x.dtype
     if out is None:
         out = torch.empty(x.shape, dtype=dtype, device=x.device)

@@ -146,3 +146,10 @@ def test_what_the_short_way_leaves_works_or_says_why():
         A.rotary(x, f, torch.zeros(2, dtype=torch.int64, device="cuda"))
     with pytest.raises(ValueError):
         A.rotary(x.transpose(1, 2).contiguous().transpose(1, 2), f)
+
+
+def test_an_output_without_its_rows_is_refused():
+    """rotary's out_other is where `other` goes: without rows to turn nothing would be written there."""
+    x, f = torch.zeros(2, 3, 128), torch.zeros(64, dtype=torch.float64)
+    with pytest.raises(ValueError, match="out_other"):
+        A.rotary(x, f, out_other=torch.empty(2, 1, 128))

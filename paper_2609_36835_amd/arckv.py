@@ -3,7 +3,7 @@
 Every function mirrors the C entry point of the same name in include/arckv.h.
 Those of the 4-bit cache and of rotary positions, which a decode step calls for every
 layer, have their arguments checked and passed on in native code (binding/bind.cpp)
-where all is as documented.
+where all is as documented, and where that code was built for this torch.
 Tensors must be CUDA (HIP) tensors, contiguous, of the documented dtype; the
 work is enqueued on torch's current stream.  Nothing here computes any part
 of the compaction: if the library is missing, loading fails loudly.
@@ -15,6 +15,7 @@ import importlib.machinery
 import importlib.util
 import math
 import os
+import warnings
 from typing import NamedTuple, Optional
 
 import torch
@@ -160,20 +161,45 @@ def lib():
 _BIND = None
 
 
-def _bind():
-    """The native short way to the entry points that decode steps call (binding/bind.cpp): each function takes the current
-    device and its namesake's arguments here, and returns None where it leaves them, and their errors, to that."""
-    global _BIND
-    if _BIND is None:
-        if not os.path.exists(BIND_PATH):
-            raise RuntimeError(f"{BIND_PATH} is missing: run `python -m paper_2609_36835_amd.build` first")
-        L = lib()
+class _LongWay:
+    """Stands in for the native module where there is none that fits, and leaves every call to its namesake here."""
+
+    @staticmethod
+    def ncache_write(*args):
+        return None
+
+    ncache_read = attend_ncache = rotary = ncache_write
+
+
+def _native():
+    """The native module, or what keeps it from use."""
+    if not os.path.exists(BIND_PATH):
+        return "is missing"
+    try:
         loader = importlib.machinery.ExtensionFileLoader("_arckv_bind", BIND_PATH)
         m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_arckv_bind", loader))
         loader.exec_module(m)
-        m.init(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            L.arckv_ncache_write, L.arckv_ncache_read, L.arckv_attend_ncache_workspace_size, L.arckv_attend_ncache,
-            L.arckv_rotary)), torch._C._cuda_getCurrentRawStream)
+    except ImportError as e:
+        return f"cannot be loaded ({e})"
+    built_for = getattr(m, "built_for", "of unknown version")
+    return m if built_for == torch.__version__ else f"was built for torch {built_for}"
+
+
+def _bind():
+    """The native short way to the entry points that decode steps call (binding/bind.cpp): each function takes the current
+    device and its namesake's arguments here, and returns None where it leaves them, and their errors, to that.  It is
+    host code that needs this very torch; without it every call goes the long way, to the same kernels."""
+    global _BIND
+    if _BIND is None:
+        L, m = lib(), _native()
+        if isinstance(m, str):
+            warnings.warn(f"{BIND_PATH} {m}: calls take some microseconds of host time more "
+                          "(`python -m paper_2609_36835_amd.build` builds it)", RuntimeWarning, stacklevel=3)
+            m = _LongWay()
+        else:
+            m.init(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
+                L.arckv_ncache_write, L.arckv_ncache_read, L.arckv_attend_ncache_workspace_size, L.arckv_attend_ncache,
+                L.arckv_rotary)), torch._C._cuda_getCurrentRawStream)
         _BIND = m
     return _BIND
 

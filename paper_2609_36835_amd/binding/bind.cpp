@@ -248,4 +248,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_arckv_bind", nullptr, -1, methods
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__arckv_bind() { return PyModule_Create(&module); }
+// built_for: the torch whose C++ types this file was compiled with; used with another it may read them wrongly.
+PyMODINIT_FUNC PyInit__arckv_bind() {
+  PyObject *m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", ARCKV_TORCH) < 0) Py_CLEAR(m);
+  return m;
+}

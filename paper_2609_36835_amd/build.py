@@ -58,6 +58,7 @@ def _compile(src: str, hipcc: str) -> str:
 
 
 def build_binding() -> str:
+    """The native part of the Python binding, for the torch that is installed."""
     import torch
     at = os.path.dirname(torch.__file__)
     cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
@@ -66,7 +67,7 @@ def build_binding() -> str:
     rocm = os.path.dirname(os.path.dirname(os.path.realpath(_hipcc())))
     tmp = BIND + ".tmp"
     cmd = [cxx, "-O2", "-fPIC", "-shared", "-std=c++17", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, "-I", os.path.join(at, "include"),
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DARCKV_TORCH="{torch.__version__}"', "-I", INCLUDE, "-I", os.path.join(at, "include"),
            "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
            "-I", os.path.join(rocm, "include"), BIND_SOURCE, "-o", tmp, "-L", os.path.join(at, "lib"), "-ltorch_python",
            "-ltorch_cpu", "-lc10"]
@@ -77,14 +78,26 @@ def build_binding() -> str:
     return BIND
 
 
+def _binding():
+    """build_binding() where a host compiler and torch's headers are at hand.  The library does without: its Python
+    binding then goes through ctypes for every call, so none that was built before is left for it to find."""
+    try:
+        return build_binding()
+    except (ImportError, OSError, RuntimeError) as e:
+        if os.path.exists(BIND):
+            os.remove(BIND)
+        print(f"{BIND} not built, calls take some microseconds of host time more: {e}", file=sys.stderr)
+        return None
+
+
 def build(verbose: bool = True, jobs: int = 8) -> str:
     hipcc = _hipcc()
     os.makedirs(BUILD_DIR, exist_ok=True)
     srcs = sources()
     with concurrent.futures.ThreadPoolExecutor(max_workers=max(1, min(jobs, len(srcs) + 1))) as ex:
-        binding = ex.submit(build_binding)
+        binding = ex.submit(_binding)
         objs = list(ex.map(lambda s: _compile(s, hipcc), srcs))
-        binding.result()
+        bound = binding.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp]
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -92,7 +105,7 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, LIB)
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources, and {BIND}", file=sys.stderr)
+        print(f"built {LIB} from {len(srcs)} sources" + (f", and {bound}" if bound else ""), file=sys.stderr)
     return LIB
 
 

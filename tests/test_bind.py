@@ -1,11 +1,13 @@
 """The binding's native short way: it leaves everything that is not as documented to the long way, whose errors say what is
 wrong, and where it takes a call it does what the long way does."""
 import math
+import os
 
 import pytest
 import torch
 
 from paper_2609_36835_amd import arckv as A
+from paper_2609_36835_amd import build as B
 
 NAMES = ("ncache_write", "ncache_read", "attend_ncache", "rotary")
 
@@ -153,3 +155,60 @@ def test_an_output_without_its_rows_is_refused():
     x, f = torch.zeros(2, 3, 128), torch.zeros(64, dtype=torch.float64)
     with pytest.raises(ValueError, match="out_other"):
         A.rotary(x, f, out_other=torch.empty(2, 1, 128))
+
+
+def test_the_library_is_built_without_a_host_compiler(monkeypatch, tmp_path, capfd):
+    """hipcc alone makes the library; a native part that an earlier build left does not stay beside it."""
+    stale = tmp_path / "_arckv_bind.so"
+    stale.write_bytes(b"stale")
+    monkeypatch.setenv("CXX", str(tmp_path / "no-compiler"))
+    monkeypatch.setattr(B, "BIND", str(stale))
+    monkeypatch.setattr(B, "LIB", str(tmp_path / "libarckv.so"))
+    monkeypatch.setattr(B, "BUILD_DIR", str(tmp_path / "objects"))
+    monkeypatch.setattr(B, "sources", lambda: [os.path.join(B.CSRC, "util.hip")])
+    assert B.build() == B.LIB and os.path.exists(B.LIB)
+    assert not stale.exists()
+    assert "no-compiler" in capfd.readouterr().err
+
+
+def unfit(monkeypatch, tmp_path, why):
+    monkeypatch.setattr(A, "_BIND", None)
+    if why == "another torch's":
+        monkeypatch.setattr(torch, "__version__", "0.1")
+        return
+    path = tmp_path / "_arckv_bind.so"
+    if why == "no library":
+        path.write_bytes(b"not one")
+    monkeypatch.setattr(A, "BIND_PATH", str(path))
+
+
+@pytest.mark.parametrize("why", ["missing", "no library", "another torch's"])
+def test_without_a_native_part_that_fits_all_calls_go_the_long_way(monkeypatch, tmp_path, why):
+    unfit(monkeypatch, tmp_path, why)
+    with pytest.warns(RuntimeWarning, match="_arckv_bind.so"):
+        m = A._bind()
+    assert m is A._bind()
+    for name in NAMES:
+        assert getattr(m, name)(0, 1, 2) is None
+    monkeypatch.undo()
+    assert A._bind() is not m
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("why", ["missing", "no library", "another torch's"])
+def test_calls_work_without_a_native_part(monkeypatch, tmp_path, why):
+    x, f = torch.randn(3, 20, 128, device="cuda").bfloat16(), A.rotary_frequencies(64)
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")
+
+    def calls():
+        c = A.ncache(3, 30)
+        for t in c:
+            t.zero_()
+        y = A.rotary(x, f, pos)
+        A.ncache_write(c, y, x)
+        return (y, *c, *A.ncache_read(c, 2, 9), A.attend_ncache(x[:, :4].contiguous(), c))
+    want = calls()
+    unfit(monkeypatch, tmp_path, why)
+    with pytest.warns(RuntimeWarning):
+        got = calls()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))

@@ -24,6 +24,16 @@ PyObject *stream_of_;
 
 PyObject *long_way() { Py_RETURN_NONE; }
 
+// The interpreter's lock is open while one of these lives: a launch may wait for room in a queue, an allocation for the GPU.
+struct Unlocked {
+  PyThreadState *state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+template <typename F> auto unlocked(F f) {
+  Unlocked u;
+  return f();
+}
+
 // The current device's tensor behind an argument; null for anything else.
 const at::Tensor *tensor(PyObject *o, int64_t dev) {
   if (!THPVariable_Check(o)) return nullptr;
@@ -98,7 +108,9 @@ PyObject *ncache_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
       !pointer_or_none(a[4], dev, at::kInt, {c.P}, &start) || !pointer_or_none(a[5], dev, at::kInt, {c.P}, &count))
     return long_way();
   if (!stream(a[0], &s)) return nullptr;
-  if (ncache_write_(&c, (int32_t)rows, dtype, k, v, (const int32_t *)start, (const int32_t *)count, s) != ARCKV_OK) return long_way();
+  if (unlocked([&] { return ncache_write_(&c, (int32_t)rows, dtype, k, v, (const int32_t *)start, (const int32_t *)count, s); }) !=
+      ARCKV_OK)
+    return long_way();
   Py_RETURN_TRUE;
   END_HANDLE_TH_ERRORS
 }
@@ -122,10 +134,14 @@ PyObject *ncache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
   hipStream_t s;
   if (!stream(a[0], &s)) return nullptr;
   const auto options = THPVariable_Unpack(PyTuple_GET_ITEM(a[1], 0)).options().dtype(type);
-  at::Tensor K = at::empty({c.P, rows, 128}, options), V = at::empty({c.P, rows, 128}, options);
-  if (ncache_read_(&c, first, rows, type == at::kFloat ? ARCKV_F32 : ARCKV_BF16, (const int32_t *)length, K.data_ptr(), V.data_ptr(),
-                   s) != ARCKV_OK)
-    return long_way();
+  at::Tensor K, V;
+  const arckv_status got = unlocked([&] {
+    K = at::empty({c.P, rows, 128}, options);
+    V = at::empty({c.P, rows, 128}, options);
+    return ncache_read_(&c, first, rows, type == at::kFloat ? ARCKV_F32 : ARCKV_BF16, (const int32_t *)length, K.data_ptr(),
+                        V.data_ptr(), s);
+  });
+  if (got != ARCKV_OK) return long_way();
   PyObject *k = THPVariable_Wrap(std::move(K)), *v = THPVariable_Wrap(std::move(V));
   PyObject *both = k && v ? PyTuple_Pack(2, k, v) : nullptr;
   Py_XDECREF(k);
@@ -167,18 +183,22 @@ PyObject *attend_ncache(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (a[9] != Py_None && !pointer(a[9], dev, at::kFloat, {c.P, G, 128}, &o)) return long_way();
   hipStream_t s;
   if (!stream(a[0], &s)) return nullptr;
-  at::Tensor out, space;
-  if (a[9] == Py_None) {
-    out = at::empty({c.P, G, 128}, Q->options().dtype(at::kFloat));
-    o = out.data_ptr();
-  }
-  if (!w && bytes) {   // torch's device allocations are 512-byte aligned
-    space = at::empty({(int64_t)bytes}, Q->options().dtype(at::kByte));
-    w = space.data_ptr();
-  }
-  if (attend_ncache_(&c, (int32_t)G, (int32_t)F, (float)scale, q, (const float *)beta, (const int32_t *)length, kf, vf,
-                     (const int32_t *)length_f, (float *)o, w, bytes, s) != ARCKV_OK)
-    return long_way();
+  at::Tensor out;
+  const bool new_out = a[9] == Py_None;
+  const arckv_status got = unlocked([&] {
+    at::Tensor space;
+    if (new_out) {
+      out = at::empty({c.P, G, 128}, Q->options().dtype(at::kFloat));
+      o = out.data_ptr();
+    }
+    if (!w && bytes) {   // torch's device allocations are 512-byte aligned
+      space = at::empty({(int64_t)bytes}, Q->options().dtype(at::kByte));
+      w = space.data_ptr();
+    }
+    return attend_ncache_(&c, (int32_t)G, (int32_t)F, (float)scale, q, (const float *)beta, (const int32_t *)length, kf, vf,
+                          (const int32_t *)length_f, (float *)o, w, bytes, s);
+  });
+  if (got != ARCKV_OK) return long_way();
   if (a[9] == Py_None) return THPVariable_Wrap(std::move(out));
   Py_INCREF(a[9]);
   return a[9];
@@ -217,7 +237,8 @@ PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
                                  dtype, a[6] == Py_True, (float)PyFloat_AS_DOUBLE(a[7])};
   hipStream_t s;
   if (!stream(a[0], &s)) return nullptr;
-  if (rotary_(&p, (const int32_t *)positions, (const double *)freq, &r[0], a[4] != Py_None ? &r[1] : nullptr, s) != ARCKV_OK)
+  const arckv_rotary_rows *other = a[4] != Py_None ? &r[1] : nullptr;
+  if (unlocked([&] { return rotary_(&p, (const int32_t *)positions, (const double *)freq, &r[0], other, s); }) != ARCKV_OK)
     return long_way();
   Py_RETURN_TRUE;
   END_HANDLE_TH_ERRORS

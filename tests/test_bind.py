@@ -1,5 +1,7 @@
 """The binding's native short way: it leaves everything that is not as documented to the long way, whose errors say what is
 wrong, and where it takes a call it does what the long way does."""
+import concurrent.futures
+import ctypes
 import math
 import os
 
@@ -212,3 +214,49 @@ def test_calls_work_without_a_native_part(monkeypatch, tmp_path, why):
     with pytest.warns(RuntimeWarning):
         got = calls()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.gpu
+def test_the_library_is_called_without_the_interpreters_lock():
+    """A launch may wait, for room in a queue say; other Python threads go on meanwhile.  In place of each entry point stands
+    Python's own question whether this thread holds the lock: 0, which is also the entry points' OK, where it does not."""
+    m, L = A._bind(), A.lib()
+    at = lambda *f: tuple(ctypes.cast(x, ctypes.c_void_p).value for x in f)
+    held = ctypes.pythonapi.PyGILState_Check
+    c, dev = A.ncache(2, 50), torch.cuda.current_device()
+    x, f = torch.zeros(2, 3, 128, dtype=torch.bfloat16, device="cuda"), A.rotary_frequencies(64)
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    m.init(at(*[held] * 5), torch._C._cuda_getCurrentRawStream)
+    try:
+        taken = [m.ncache_write(dev, c, x, x, None, None), m.ncache_read(dev, c, 0, 3, False, None),
+                 m.attend_ncache(dev, x, c, None, None, None, None, None, None, None, ws),
+                 m.rotary(dev, x, f, None, None, False, False, 1.0, torch.empty_like(x), None)]
+    finally:
+        m.init(at(L.arckv_ncache_write, L.arckv_ncache_read, L.arckv_attend_ncache_workspace_size, L.arckv_attend_ncache,
+                  L.arckv_rotary), torch._C._cuda_getCurrentRawStream)
+    assert all(t is not None for t in taken)
+
+
+@pytest.mark.gpu
+def test_calls_from_two_threads_at_once():
+    """Each thread's calls, on a stream of its own, give what they give alone."""
+    x = [torch.randn(6, 200, 128, device="cuda").bfloat16() for _ in range(2)]
+    f = A.rotary_frequencies(64)
+
+    def calls(i):
+        out = []
+        with torch.cuda.stream(streams[i]):
+            for _ in range(50):
+                c = A.ncache(6, 200)
+                y = A.rotary(x[i], f)
+                A.ncache_write(c, y, x[i])
+                out = [y, *A.ncache_read(c), A.attend_ncache(x[i][:, :4].contiguous(), c)]
+        streams[i].synchronize()
+        return out
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    want = [calls(0), calls(1)]
+    with concurrent.futures.ThreadPoolExecutor(2) as ex:
+        got = list(ex.map(calls, (0, 1)))
+    for a, b in zip(want, got):
+        assert all(torch.equal(s, t) for s, t in zip(a, b))

@@ -468,17 +468,26 @@ __global__ void __launch_bounds__(64 * W, W == kAnW ? 3 : 2) k_attendn_partial(A
 
 int units_of(int rows, int F) { return (rows + kAnBlock - 1) / kAnBlock + (F + kAttendTail - 1) / kAttendTail; }
 
+// Waves of a workgroup.  A pair that is one workgroup's and has a CU to itself takes eight, two to a SIMD, where four would
+// go round more than once.  us with 4 and with 8: 8 pairs of 819 + 37 rows 8.4 and 7.9, of 300 5.8 and 5.6; 64 of 1500 9.1 and 8.6;
+// 200 of 600 + 64 for 16 queries 10.8 and 9.5; 256 of 4000 26.5 and 24.7.  Where four do not go round, more only wait: 300 of 60
+// 5.2 and 7.5; of several chunks too: 8 of 2000 7.5 and 9.7.
+int waves_of(int P, int units, int nch) { return nch == 1 && P <= kAnCus && units > kAnW ? kAnMore : kAnW; }
+
 }  // namespace
 
 // Chunks per pair, by the time that a call of as many takes, in ns: up to three workgroups run at a time on each of 256 CUs
 // (the fullest ends the call), which share the memory's rate but need a wave's latency for each unit all the same; a
-// workgroup's start, beside others on its CU; the second launch, which joins.
-// us per call by chunks: 512 pairs of 3277 + 256 rows 1: 50.3, 2: 52.5, 3: 53.9; of 8192-16384 rows 1: 139.5, 2: 148.8, 3: 145.5; 256
-// of 4500-9000 1: 51.7, 2: 47.3, 3: 45.6; of 4000 1: 26.5, 2: 28.2; 64 of 2500 1: 12.8, 2: 11.4, 4: 10.4, 8: 12.7; 8 of 131072 21:
-// 41.7, 32: 34.7, 64: 33.0, 86: 35.7; of 4000 1: 17.7, 4: 10.3, 16: 8.6; of 819 + 37 1: 8.6, 2: 9.3, 4: 9.1; one of 131072 32: 20.8,
-// 64: 15.2, 128: 14.0, 256: 16.5.
+// workgroup's start, beside others on its CU; the second launch, which joins.  One chunk that eight waves take is priced as such
+// where that is less.
+// us per call by chunks: 512 pairs of 3277 + 256 rows 1: 49.3, 2: 50.5, 3: 52.2; of 8192-16384 rows 1: 139.2, 2: 148.1, 3: 144.3;
+// eight waves' one chunk and others': 256 of 4500-9000 1: 43.4, 2: 45.8, 3: 44.6; of 4000 1: 24.9, 2: 27.4; 200 of 6621 1: 34.2, 2:
+// 38.4, for 16 queries 40.5 and 45.7; 160 of 2500 1: 13.3, 2: 16.9, 3: 15.2; of 46849 1: 202, 2: 216, 3: 165; 64 of 2500 1: 11.6, 2: 11.6,
+// 4: 10.8, 8: 12.6; 8 of 4000 1: 15.2, 4: 10.5, 16: 10.2; of 819 + 37 1: 8.2, 2: 10.0, 4: 9.9; 8 of 131072 21: 39.2, 32: 30.0, 64: 29.6,
+// 86: 30.5; one of 131072 32: 20.6, 64: 15.1, 128: 14.0, 256: 17.1.
 int attendn_chunks(int P, int rows, int F) {
-  constexpr int64_t kAlone = 1000, kLatency = 1600, kShare = 1400, kStart = 3500, kMore = 1000, kJoin = 3000, kJoinChunk = 30;
+  constexpr int64_t kAlone = 1000, kLatency = 1600, kShare = 1400, kStart = 3500, kMore = 1000, kJoin = 3000, kJoinChunk = 30,
+                    kEight = 1600;   // eight waves' units: their latency, and the pairs' share of the memory's rate
   const int units = units_of(rows, F);
   const int n = (units + kAnW - 1) / kAnW;
   int best = 1;
@@ -488,8 +497,9 @@ int attendn_chunks(int P, int rows, int F) {
     const int units_each = (n + c - 1) / c;
     const int64_t wgs = (int64_t)P * c, rounds = (wgs + kAnSlots - 1) / kAnSlots;
     const int64_t on_cu = min((wgs + kAnCus - 1) / kAnCus, kAnSlots / kAnCus);
-    const int64_t unit = wgs <= kAnCus / 2 ? kAlone : max(kLatency, kShare * on_cu);
-    const int64_t cost = rounds * (units_each * unit + kStart + kMore * (on_cu - 1)) + (c > 1 ? kJoin + kJoinChunk * c : 0);
+    int64_t blocks = units_each * (wgs <= kAnCus / 2 ? kAlone : max(kLatency, kShare * on_cu));
+    if (waves_of(P, units, c) == kAnMore) blocks = min(blocks, (units + kAnMore - 1) / kAnMore * (kEight + kShare * P / kAnCus));
+    const int64_t cost = rounds * (blocks + kStart + kMore * (on_cu - 1)) + (c > 1 ? kJoin + kJoinChunk * c : 0);
     if (cost < least) {
       least = cost;
       best = c;
@@ -508,11 +518,7 @@ hipError_t launch_attendn(const NCache &c, int G, int F, float scale, const void
   // pairs over y and z: a grid's y extent is limited
   const unsigned py = (unsigned)min(c.P, 32768), pz = (unsigned)((c.P + 32767) / 32768);
   const bool stream = (int64_t)c.P * c.rows * 2 * kNRow > kAnKept;
-  // A pair that is one workgroup's and has a CU to itself takes eight waves, two to a SIMD, where four would go round more than
-  // once.  us with 4 and with 8: 8 pairs of 819 + 37 rows 8.4 and 7.9, of 300 5.8 and 5.6; 64 of 1500 9.1 and 8.6; 200 of 600 + 64
-  // for 16 queries 10.8 and 9.5; 256 of 4000 26.5 and 24.7.  Where four do not go round, more only wait: 300 of 60 5.2 and 7.5; of
-  // several chunks too: 8 of 2000 7.5 and 9.7.
-  const int waves = nch == 1 && c.P <= kAnCus && units_of(c.rows, F) > kAnW ? kAnMore : kAnW;
+  const int waves = waves_of(c.P, units_of(c.rows, F), nch);
   auto go = [&](auto kern) {
     hipLaunchKernelGGL(kern, dim3((unsigned)a.nch, py, pz), dim3(64 * waves), 0, s, a);
     return hipGetLastError();

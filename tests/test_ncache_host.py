@@ -176,3 +176,14 @@ def test_host_code_under_sanitizers():
                UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1", HIP_VISIBLE_DEVICES="")
     r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
     assert r.returncode == 0 and "ok: 0 failures" in r.stdout, (r.stdout[-4000:], r.stderr[-4000:])
+
+
+def test_chunks_by_the_kernel_that_runs():
+    """A pair that eight waves take whole in less time than several chunks of four waves is one chunk, which needs no workspace;
+    long pairs that leave CUs without work, or many, are cut."""
+    from paper_2609_36835_amd import arckv
+    size = arckv.attend_ncache_workspace_size
+    for P, R in ((256, 9000), (224, 46849), (200, 6621), (200, 20254), (192, 4353), (160, 2500), (256, 4000), (64, 1500), (8, 819)):
+        assert size(P, R, 4) == size(P, R, 16) == 0, (P, R)
+    for P, R in ((1, 131072), (8, 131072), (8, 4000), (64, 2500), (96, 10069), (128, 10069), (160, 46849), (192, 20254), (256, 20254)):
+        assert size(P, R, 4) > 0, (P, R)

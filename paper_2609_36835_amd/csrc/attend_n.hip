@@ -7,11 +7,14 @@
 // HBM-bound: 136 bytes per token.  Split-key in two kernels:
 //   k_attendn_partial  a workgroup takes a share of the pair's units (blocks of 64 rows, 32 rows of the tail) as its lengths
 //                      say, a wave a unit at a time, with a running softmax.  The next block's keys are loaded once this
-//                      one's are used up, and so are its values: 144 to 172 registers, three waves on a SIMD.
+//                      one's are used up, and so are its values: 144 to 168 registers and three waves on a SIMD in workgroups
+//                      of four; 144 to 172 in those of eight, which have a CU to themselves, two on a SIMD.
 //   k_attend_combine   merges the partials of a pair; a call of one chunk per pair needs none.
 // 512 pairs of 3277 rows with bias and 256 tail rows take 49 us (5.9 TB/s), of 8192 to 16384 rows 140 us (6.2), of 32768 rows
-// 330 (6.9); with the loads alone, at the same places, the first two take 48.4 and 137.3.  8 pairs of 819 + 37 rows take 7.9 us: a
-// start of 3.5, a little over 1 for each of a wave's units, of which the loads' way is the lesser part, and the waves' join.
+// 330 (6.9); with the loads alone, at the same places, the first two take 48.4 and 137.3.  256 of 4096-8192 rows for 16 queries take
+// 49 us (4.5 TB/s), one workgroup a CU; vector units are busy 37% of that, matrix units 25%.  8 pairs of 819 + 37 rows take 8 us: a
+// start of 3.5, a little over 1 for each of a wave's units, and the waves' join.  A wave loads its first rows of the tail once its
+// blocks are done, so there the way to memory counts twice.
 //
 // Logits.  Keys go to MFMA 16x16x128 as they are held, codes and scales, so that nothing is unpacked.  Its other operand
 // is 8-bit, and it aligns the products of neighbouring channels to the largest of them, 13 bits below which it cuts.  So a

@@ -18,8 +18,8 @@ namespace arckv {
 namespace {
 constexpr int kRotThreads = 256;
 // Bytes above which rows are read as streams that the caches do not keep.  us kept and streamed: 4096 tokens of 40 bf16 heads (42
-// MB in) 13.9 and 16.3, 8000 (82 MB) 25.5 and 29.6, 9500 (97 MB) 33.5 and 34.6, 12000 (123 MB) 42.8 and 40.9, 32768 (336 MB) 114
-// and 107.
+// MB in) 14.0 and 17.4, 8000 (82 MB) 27.3 and 30.5, 9500 (97 MB) 34.8 and 35.8, 12000 (123 MB) 45.6 and 44.1, 32768 (336 MB) 123
+// and 113.
 constexpr int64_t kRotKept = (int64_t)96 << 20;
 // Bytes above which, if not streamed, a thread takes two rows instead of one, where tokens have more than one head (one head's rows
 // need as many angles as there are channels).  us with one, two and four: 64 tokens of 40 bf16 heads 2.8, 3.2, 3.9; 1000 (10 MB)

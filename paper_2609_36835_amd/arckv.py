@@ -182,7 +182,7 @@ def _native():
     except ImportError as e:
         return f"cannot be loaded ({e})"
     built_for = getattr(m, "built_for", "of unknown version")
-    return m if built_for == torch.__version__ else f"was built for torch {built_for}"
+    return m if built_for == str(torch.__version__) else f"was built for torch {built_for}"
 
 
 def _bind():

@@ -97,3 +97,33 @@ def test_small_values_at_many_rows():
     K_f, V_f = rows(g, P, 40, 128), rows(g, P, 40, 128) * 2.0 ** -60
     check_attend(A().attend_ncache(Q, c, None, None, K_f, V_f) * 2.0 ** 60, Q, [c[0], c[1], c[2], c[3] + 60], None, None, K_f,
                  V_f * 2.0 ** 60, None)
+
+
+@pytest.mark.parametrize("G", [1, 6, 16])
+def test_logits_of_minus_infinity(G):
+    """Rows whose logit is -inf, of an infinite key in the tail or of products beyond float32, count as left out; of +inf, the
+    query is NaN."""
+    g = np.random.default_rng(G)
+    P, R, F = 3, 200, 50
+    c = make_cache(P, R)
+    K = rows(g, P, R, 128)
+    K[0, ::3] = 0
+    K[0, ::3, 9] = -2.0 ** 120
+    K[1], K[1, :, 9] = 0, -2.0 ** 120
+    A().ncache_write(c, K, rows(g, P, R, 128))
+    Q, K_f, V_f = rows(g, P, G, 128), rows(g, P, F, 128), rows(g, P, F, 128)
+    Q[:2] = 0
+    Q[:2, :, 9] = 2.0 ** 20
+    Q[2, :, 9] = 1.0
+    K_f[:] = 0
+    K_f[2, ::2, 9] = -math.inf
+    print(f"logits of -inf G={G}", flush=True)
+    out = A().attend_ncache(Q, c)
+    beta = torch.zeros(P, R, device="cuda")
+    beta[0, ::3] = -math.inf
+    check_attend(out[:1], Q[:1], [t[:1] for t in c], beta[:1], None, None, None, None)
+    assert (out[1] == 0).all() and out[2].isfinite().all()
+    out = A().attend_ncache(Q, c, None, i32([0] * P), K_f, V_f)[2:]
+    check_attend(out, Q[2:], [t[2:] for t in c], None, [0], K_f[2:, 1::2], V_f[2:, 1::2], None)
+    K_f[2, 0, 9] = math.inf
+    assert A().attend_ncache(Q, c, None, None, K_f, V_f)[2].isnan().all()
